@@ -15,9 +15,6 @@ import torch
 
 own = False   # True: the library's entry points; False: the plain forms below
 
-if own:
-    from paper_2604_21215_amd import binding
-
 DEVICE = "cuda:0"
 MATRICES = ("Wq", "Wk", "Wv", "Wo", "W1", "W2")
 GAINS = ("g_attn", "g_mlp", "g_kv", "g_q", "g_k")
@@ -166,7 +163,7 @@ def prepare(case, seed):
 _contexts = {}
 
 
-def _context(case):
+def _context(case, binding):
     """The context that a server keeps for its layers: one per shape, whatever the batch in hand holds."""
     d, rows = case.get("d") or 64 * case["H"], case.get("S") or case["B"]
     key = (d, rows, case["dtype"], case.get("alibi", 0.0), case.get("scale", 1.0))
@@ -177,8 +174,10 @@ def _context(case):
 
 
 def _run_own(s):
+    from paper_2604_21215_amd import binding
+
     case = s["case"]
-    ctx, kind = _context(case), case["kind"]
+    ctx, kind = _context(case, binding), case["kind"]
     if kind == "readout":
         ctx.rt_lm_head_mx4(s["codes"], s["exps"], s["g_final"], s["z"], case["d"], case["B"], s["logits"])
         return s["logits"]
