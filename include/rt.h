@@ -100,6 +100,7 @@ typedef struct {
 } rt_config;
 #define RT_RESERVE_LOOP_FREE 0x1u /* rt_layer_recompute, rt_transformer_layer, rt_layer_prefill_blocked */
 #define RT_RESERVE_BACKWARD 0x2u  /* rt_layer_backward */
+#define RT_RESERVE_PAGED 0x4u     /* rt_paged_attention, rt_decode_step_paged */
 
 /* Device pointers, caller-owned, read-only.  Matrices are row-major [out, in] (y = W u).
  * Gains: NULL = ones.  g_kv NULL = use g_attn.  g_q, g_k are [d_model] = [n_heads, head_dim]. */
@@ -281,6 +282,80 @@ rt_status rt_embed_rows(rt_ctx *ctx, const void *table, int32_t vocab, const int
 rt_status rt_lm_head(rt_ctx *ctx, const void *W_lm, const void *g_final, int32_t vocab, const void *z, int64_t z_stride,
                      int32_t B, float *logits);
 
+/* Serving a batch whose sequences have lengths of their own: the persistent pairs of every sequence lie in pages of page_len positions
+ * that any sequence's line of a page table may name, in the storage dtype or in eight bits.  All pointers are device pointers, the
+ * numbers in table, first, count, lens and pos are read on the device: they may change between replays of a captured call, while
+ * the sizes passed by value bound them.  None of these calls is limited by max_seq (a context for them alone needs max_seq = 1).
+ *   8 bits: a row of 64 values u (one position, one head) is held as codes c = round(u / 2^e), ties to even, |c| <= 127, with the
+ *   smallest e >= -126 for which every value fits, and the byte e + 127; it reads as c 2^e, off by at most 2^e / 2 <= max |u| / 127,
+ *   exactly representable in bf16.  Byte 0: a row of zeros.  Byte 255: a value was not finite; the row reads as NaN.
+ *   A table entry outside [0, pages) names no page: it is never followed.  Rows written there are dropped, rows read from there are
+ *   NaN, an attention over it gives a row of NaN.  Entries past a sequence's last position are not looked at. */
+typedef struct {
+    void *K, *V;              /* [pages][n_heads][page_len][head_dim]: storage dtype, or int8 codes (bits = 8); on 16 bytes */
+    uint8_t *K_exp, *V_exp;   /* [pages][n_heads][page_len] bytes of a cache of 8 bits, else NULL */
+    const int32_t *table;     /* [S][table_stride]: entry i of sequence s is the page of positions i page_len .. + page_len - 1 */
+    int64_t table_stride;     /* entries; table_stride * page_len positions at most */
+    int32_t pages;
+    int32_t page_len;         /* a power of two, 16 .. 1024 */
+    int32_t bits;             /* 0: storage dtype; 8 */
+} rt_paged_cache;
+
+/* Rows of pairs into their pages: positions first[s] .. first[s] + count[s] - 1 of sequence s take rows n = 0 .. count[s] - 1 of k, v.
+ *   k, v: row (s, n) of [n_heads][head_dim] elements of the storage dtype at s * seq_stride + n * pos_stride elements (multiples of 16
+ *   bytes, at least d_model): seq_stride = d_model, pos_stride = B d_model for the caches of rt_layer_prefill and rt_decode_step.
+ *   count[s] is cut to [0, N]; count NULL = N for every sequence.  first[s] < 0: an idle place, nothing is written for it.  Positions
+ *   past table_stride * page_len are dropped.  Two rows of one call that name the same place race.
+ *   1 <= S <= 65535, 1 <= N <= 2^20, N n_heads <= 2^30.  No scratch is used; S is not limited by max_batch. */
+rt_status rt_cache_write(rt_ctx *ctx, const rt_paged_cache *cache, int32_t S, const int32_t *first, const int32_t *count, int32_t N,
+                         const void *k, const void *v, int64_t seq_stride, int64_t pos_stride);
+
+/* The same rows back, in the storage dtype.  Rows at and past count[s], and those of idle places, are left as they were; positions past
+ * table_stride * page_len read as NaN. */
+rt_status rt_cache_read(rt_ctx *ctx, const rt_paged_cache *cache, int32_t S, const int32_t *first, const int32_t *count, int32_t N,
+                        void *k, void *v, int64_t seq_stride, int64_t pos_stride);
+
+/* Attention of one new token per sequence (Sec. 2, Notation, with this context's attn_scale and ALiBi bias): the query q_s, at position
+ * lens[s], over the cached rows 0 .. lens[s] - 1 of sequence s and, if given, the token's own temporary pair at distance 0.
+ *   q [S rows][d_model] storage dtype, q_stride elements apart (at least d_model); k_t, v_t the same, kv_stride apart, both or neither.
+ *   out: rows out_stride elements apart, written in the storage dtype; lse [S][n_heads] fp32 or NULL: log sum exp of the row's logits.
+ *   lens[s] < 0: an idle place of a padded batch, its rows of out and lse are left as they were.  No cached row and no pair, or no logit
+ *   above minus infinity: out 0, lse minus infinity.  lens[s] > max_len: NaN.
+ *   1 <= S <= max_batch, 0 <= max_len <= min(2^20, table_stride * page_len); the work is laid out for max_len.
+ *   fp32 sums and softmax.  Results do not depend on other sequences of the call but for max_len and S, by which the cache is cut into
+ *   parts whose softmax states are joined in their order: equal calls give equal bits.
+ *   The first call allocates scratch (18 MB, kept until rt_destroy) unless RT_RESERVE_PAGED reserved it at rt_create; a call on a stream that
+ *   is being captured needs it beforehand (RT_ERR_STATE).  A captured call uses the context's scratch at every replay: in order with the
+ *   context's other calls. */
+rt_status rt_paged_attention(rt_ctx *ctx, const rt_paged_cache *cache, int32_t S, const int32_t *lens, int32_t max_len, const void *q,
+                             int64_t q_stride, const void *k_t, const void *v_t, int64_t kv_stride, void *out, int64_t out_stride,
+                             float *lse);
+
+/* rt_decode_step for sequences at positions of their own over pages: x_t, y_t [S, d]; pos[s] (0-based) is the position of the new token,
+ * rows 0 .. pos[s] - 1 of sequence s are cached, row pos[s] is written (from fp32, rounded once: to the storage dtype or to 8 bits).
+ *   pos[s] < 0: an idle place: its row of y_t and its pages are left as they were (its row of x_t is read).  pos[s] > max_pos: its row of
+ *   y_t is NaN, no page is written.
+ *   Two sequences that share pages of earlier positions (a common prefix) are fine; row pos[s] must lie in a page of its own.
+ *   x_t and y_t must not overlap each other or the cache.  1 <= S <= max_batch, 0 <= max_pos < min(2^20 + 1, table_stride * page_len).
+ *   Ordinary launches (seven or eight): the products of rt_decode_step's launches between rt_paged_attention's kernels.  q and the temporary pair stay in fp32.
+ *   Scratch, capture: as rt_paged_attention. */
+rt_status rt_decode_step_paged(rt_ctx *ctx, const rt_layer_weights *w, const rt_paged_cache *cache, const void *x_t, int32_t S,
+                               const int32_t *pos, int32_t max_pos, void *y_t);
+
+/* Host-only: weights in 4 bits (the MX format: blocks of 32 along a row share a scale 2^e, elements are a sign and one of 0, 1/2, 1, 3/2,
+ * 2, 3, 4, 6).  W [rows, cols] row-major in host memory, dtype RT_F32 or RT_BF16; cols a multiple of 32.
+ *   codes [rows][cols / 2]: two elements a byte, the even index in the low half; exps [rows][cols / 32]: e + 127, 1 <= e + 127 <= 254.
+ *   Of the smallest scale that reaches the block's largest weight and the one below it, the one with the smaller squared error; elements
+ *   to the nearest code, ties to the even one.  RT_ERR_INVALID_ARG also where a weight is not finite. */
+rt_status rt_mx4_pack(const void *W, int32_t dtype, int64_t rows, int32_t cols, uint8_t *codes, uint8_t *exps);
+
+/* rt_lm_head with such a matrix: logits[b, v] = < W4[v, :], RMS(z_b; g_final) >, fp32 accuracy for the weights as they are packed.
+ *   codes [vocab][d / 2] (on 16 bytes), exps [vocab][d / 32] device; a scale byte of 0 or 255 makes its row's logits NaN,
+ *   a weight past fp32's range counts as infinite.  Other arguments
+ *   as rt_lm_head; d_model <= 25856; logits must not overlap an input. */
+rt_status rt_lm_head_mx4(rt_ctx *ctx, const uint8_t *codes, const uint8_t *exps, const void *g_final, int32_t vocab, const void *z,
+                         int64_t z_stride, int32_t B, float *logits);
+
 /* Waits for nothing: the caller synchronises the stream first.  Frees scratch.  NULL is allowed. */
 rt_status rt_destroy(rt_ctx *ctx);
 
@@ -298,7 +373,7 @@ uint64_t rt_workspace_bytes(const rt_ctx *ctx);
 int32_t rt_device_wait_expired(rt_ctx *ctx);
 
 /* Name of the engine the last call on this context used: "stepwise" (also where an fp32 rt_layer_prefill runs as one cooperative
- * launch), "stepwise+graph", "persistent", "position-batched", "wavefront" (rt_stack_prefill), "decode-single-launch", "recompute",
+ * launch), "stepwise+graph", "persistent", "position-batched", "wavefront" (rt_stack_prefill), "decode-single-launch", "decode-paged", "recompute",
  * "transformer", "blocked", "backward", or "" before the first call. */
 const char *rt_engine_name(const rt_ctx *ctx);
 

@@ -21,13 +21,14 @@ RT_FLAG_ENGINE_PERSISTENT = 0x4
 RT_FLAG_NO_MFMA = 0x8
 RT_FLAG_HIP_GRAPH = 0x10
 RT_FLAG_DEBUG_POISON = 0x20
-RT_RESERVE_LOOP_FREE, RT_RESERVE_BACKWARD = 0x1, 0x2
+RT_RESERVE_LOOP_FREE, RT_RESERVE_BACKWARD, RT_RESERVE_PAGED = 0x1, 0x2, 0x4
 
 EXPORTS = ("rt_create", "rt_layer_prefill", "rt_decode_step", "rt_destroy", "rt_last_error", "rt_status_string",
            "rt_workspace_bytes", "rt_device_wait_expired", "rt_engine_name", "rt_engine_form", "rt_schedule_events", "rt_partial_slot",
            "rt_version", "rt_phase_trace", "rt_schedule_events_shifted", "rt_embed_rows", "rt_lm_head", "rt_cross_block_event",
            "rt_stack_prefill", "rt_schedule_events_chunked", "rt_layer_recompute", "rt_transformer_layer",
-           "rt_layer_prefill_blocked", "rt_decode_step_static", "rt_layer_backward", "rt_decode_phase_trace")
+           "rt_layer_prefill_blocked", "rt_decode_step_static", "rt_layer_backward", "rt_decode_phase_trace",
+           "rt_cache_write", "rt_cache_read", "rt_paged_attention", "rt_decode_step_paged", "rt_mx4_pack", "rt_lm_head_mx4")
 
 
 class rt_config(C.Structure):
@@ -46,6 +47,11 @@ class rt_layer_weights(C.Structure):
 
 class rt_layer_grads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("Wq", "Wk", "Wv", "Wo", "W1", "W2", "g_attn", "g_mlp", "g_kv", "g_q", "g_k")]
+
+
+class rt_paged_cache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("K_exp", C.c_void_p), ("V_exp", C.c_void_p), ("table", C.c_void_p),
+                ("table_stride", C.c_int64), ("pages", C.c_int32), ("page_len", C.c_int32), ("bits", C.c_int32)]
 
 
 class RTError(RuntimeError):
@@ -132,6 +138,19 @@ def load():
     L.rt_layer_backward.argtypes = [ctxp, C.POINTER(rt_layer_weights), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.POINTER(rt_layer_grads)]
     L.rt_layer_backward.restype = C.c_int
+    cachep = C.POINTER(rt_paged_cache)
+    for fn in (L.rt_cache_write, L.rt_cache_read):
+        fn.argtypes = [ctxp, cachep, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64]
+        fn.restype = C.c_int
+    L.rt_paged_attention.argtypes = [ctxp, cachep, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                     C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+    L.rt_paged_attention.restype = C.c_int
+    L.rt_decode_step_paged.argtypes = [ctxp, C.POINTER(rt_layer_weights), cachep, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]
+    L.rt_decode_step_paged.restype = C.c_int
+    L.rt_mx4_pack.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]
+    L.rt_mx4_pack.restype = C.c_int
+    L.rt_lm_head_mx4.argtypes = [ctxp, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]
+    L.rt_lm_head_mx4.restype = C.c_int
     _lib = L
     return L
 
@@ -168,6 +187,44 @@ def make_weights(w: dict) -> rt_layer_weights:
         t = w.get(name)
         setattr(s, name, None if t is None else t.data_ptr())
     return s
+
+
+def make_cache(K, V, table, K_exp=None, V_exp=None) -> rt_paged_cache:
+    """K, V [pages, H, page_len, 64] (storage dtype, or int8 with the bytes K_exp, V_exp [pages, H, page_len]), table int32 [S, entries]."""
+    for t in (K, V, K_exp, V_exp):
+        if t is not None and not t.is_contiguous():
+            raise RTError("RT_ERR_INVALID_ARG", "the arrays of a cache are contiguous")
+    if K.shape != V.shape or K.dim() != 4 or K.dtype != V.dtype or any(e is not None and e.shape != K.shape[:3] for e in (K_exp, V_exp)):
+        raise RTError("RT_ERR_INVALID_ARG", "K, V [pages, H, page_len, 64] and, in 8 bits, K_exp, V_exp [pages, H, page_len]")
+    if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1) or table.element_size() != 4:
+        raise RTError("RT_ERR_INVALID_ARG", "table is int32 [S, entries]")
+    return rt_paged_cache(K.data_ptr(), V.data_ptr(), None if K_exp is None else K_exp.data_ptr(), None if V_exp is None else V_exp.data_ptr(),
+                          table.data_ptr(), table.stride(0) if table.shape[0] > 1 else table.shape[1], K.shape[0], K.shape[2],
+                          8 if K.element_size() == 1 else 0)
+
+
+def _pair_strides(k, v):
+    """k, v [S, N, H, 64] with the same strides and the last two dimensions contiguous -> (seq_stride, pos_stride)."""
+    S, N, H, dh = k.shape
+    strides = lambda t: (t.stride(0) if S > 1 else 0, t.stride(1) if N > 1 else 0, t.stride(2) if H > 1 else dh, t.stride(3))  # noqa: E731
+    if v.shape != k.shape or strides(v) != strides(k) or strides(k)[2:] != (dh, 1):
+        raise RTError("RT_ERR_INVALID_ARG", "k and v are [S, N, H, 64] with equal strides and contiguous heads")
+    return strides(k)[:2]
+
+
+def rt_mx4_pack(W):
+    """W [rows, cols] on the host (numpy float32, or uint16 bf16 bits) -> (codes [rows, cols / 2], exps [rows, cols / 32]) uint8."""
+    import numpy as np
+    W = np.ascontiguousarray(W)
+    if W.ndim != 2 or W.dtype not in (np.float32, np.uint16):
+        raise RTError("RT_ERR_INVALID_ARG", "W is [rows, cols] float32 or uint16 (bf16 bits)")
+    rows, cols = W.shape
+    codes, exps = np.empty((rows, cols // 2), dtype=np.uint8), np.empty((rows, max(cols // 32, 1)), dtype=np.uint8)
+    L = load()
+    rc = L.rt_mx4_pack(W.ctypes.data, RT_F32 if W.dtype == np.float32 else RT_BF16, rows, cols, codes.ctypes.data, exps.ctypes.data)
+    if rc != RT_OK:
+        raise RTError(L.rt_status_string(rc).decode(), "rt_mx4_pack: cols a multiple of 32 and finite weights are required")
+    return codes, exps
 
 
 def _events(fn, N, p_min):
@@ -286,6 +343,41 @@ class RTContext:
     def rt_lm_head(self, W_lm, g_final, z, z_stride, B, logits):
         rc = self._L.rt_lm_head(self._ctx, _ptr(W_lm), _ptr(g_final), W_lm.shape[0], _ptr(z), int(z_stride), int(B),
                                 _ptr(logits))
+        _check(self._L, self._ctx, rc)
+
+    # -- rt_cache_write(ctx, cache, S, first[S] int32, count[S] int32 | None, N, k[S,N,H,64], v, seq_stride, pos_stride)
+    def rt_cache_write(self, cache: rt_paged_cache, first, count, k, v):
+        rc = self._L.rt_cache_write(self._ctx, C.byref(cache), k.shape[0], _ptr(first), _ptr(count), k.shape[1], _ptr(k), _ptr(v),
+                                    *_pair_strides(k, v))
+        _check(self._L, self._ctx, rc)
+
+    # -- rt_cache_read(ctx, cache, S, first[S] int32, count[S] int32 | None, N, k[S,N,H,64], v, seq_stride, pos_stride)
+    def rt_cache_read(self, cache: rt_paged_cache, first, count, k, v):
+        rc = self._L.rt_cache_read(self._ctx, C.byref(cache), k.shape[0], _ptr(first), _ptr(count), k.shape[1], _ptr(k), _ptr(v),
+                                   *_pair_strides(k, v))
+        _check(self._L, self._ctx, rc)
+
+    # -- rt_paged_attention(ctx, cache, S, lens[S] int32, max_len, q[S,H,64], q_stride, k_t | None, v_t | None, kv_stride, out, out_stride, lse[S,H] f32 | None)
+    def rt_paged_attention(self, cache: rt_paged_cache, lens, max_len, q, k_t, v_t, out, lse=None):
+        """q, k_t, v_t, out [S, H, 64] (or [S, d]): rows at their first stride, contiguous inside."""
+        S, d = q.shape[0], self.cfg.d_model
+        stride = lambda t: t.stride(0) if S > 1 else d  # noqa: E731
+        if k_t is not None and v_t is not None and stride(k_t) != stride(v_t):
+            raise RTError("RT_ERR_INVALID_ARG", "k_t and v_t have one stride")
+        rc = self._L.rt_paged_attention(self._ctx, C.byref(cache), S, _ptr(lens), int(max_len), _ptr(q), stride(q), _ptr(k_t), _ptr(v_t),
+                                        stride(k_t) if k_t is not None else d, _ptr(out), stride(out), _ptr(lse))
+        _check(self._L, self._ctx, rc)
+
+    # -- rt_decode_step_paged(ctx, w, cache, x_t[S,d], S, pos[S] int32, max_pos, y_t[S,d])
+    def rt_decode_step_paged(self, weights: rt_layer_weights, cache: rt_paged_cache, x_t, pos, max_pos, y_t):
+        rc = self._L.rt_decode_step_paged(self._ctx, C.byref(weights), C.byref(cache), _ptr(x_t), x_t.shape[0], _ptr(pos), int(max_pos),
+                                          _ptr(y_t))
+        _check(self._L, self._ctx, rc)
+
+    # -- rt_lm_head_mx4(ctx, codes[vocab,d/2], exps[vocab,d/32], g_final[d] | None, vocab, z rows, z_stride, B, logits[B,vocab] f32)
+    def rt_lm_head_mx4(self, codes, exps, g_final, z, z_stride, B, logits):
+        rc = self._L.rt_lm_head_mx4(self._ctx, _ptr(codes), _ptr(exps), _ptr(g_final), codes.shape[0], _ptr(z), int(z_stride), int(B),
+                                    _ptr(logits))
         _check(self._L, self._ctx, rc)
 
     # -- rt_cross_block_event(ctx, K, V, B, t1, P, nq)

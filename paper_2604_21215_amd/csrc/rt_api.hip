@@ -8,6 +8,9 @@
 #include "rt_backward.h"
 #include "rt_side_streams.h"
 #include "rt_launch_order.h"
+#include "rt_paged.h"
+#include "rt_paged_args.h"
+#include "rt_mx4.h"
 
 #include <cstdio>
 #include <cstdlib>
@@ -55,6 +58,8 @@ struct rt_ctx {
     void *bw_slab = nullptr;         // scratch of rt_layer_backward
     BwpState bw_loop;                // its single-launch reverse loop
     size_t bw_bytes = 0;
+    void *paged_slab = nullptr;      // partial states of the paged attention, then the new output rows of a paged step
+    size_t paged_bytes = 0;
     // cached HIP graph of one stepwise prefill
     hipGraphExec_t graph_exec = nullptr;
     hipStream_t capture_stream = nullptr;  // the legacy default stream cannot be captured
@@ -301,6 +306,29 @@ static rt_status ensure_backward_scratch(rt_ctx *c)
     return RT_OK;
 }
 
+static size_t paged_rows_offset() { return align_up(paged_partials_bytes(), 256); }
+static rt_status ensure_paged_scratch(rt_ctx *c)
+{
+    if (c->paged_slab) return RT_OK;
+    hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+    if (c->stream && hipStreamIsCapturing(c->stream, &capturing) != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(c, RT_ERR_HIP, "hipStreamIsCapturing failed%s");
+    }
+    if (capturing != hipStreamCaptureStatusNone)
+        return fail(c, RT_ERR_STATE, "a captured call needs the paged scratch beforehand (RT_RESERVE_PAGED or an earlier call)%s");
+    const size_t E = c->cfg.dtype == RT_BF16 ? 2 : 4;
+    const size_t need = paged_rows_offset() + (size_t)c->cfg.max_batch * c->cfg.d_model * E;
+    hipError_t e = hipMalloc(&c->paged_slab, need);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        c->paged_slab = nullptr;
+        return fail(c, e == hipErrorOutOfMemory ? RT_ERR_OOM : RT_ERR_HIP, "paged scratch: %s", hipGetErrorString(e));
+    }
+    c->paged_bytes = need;
+    return RT_OK;
+}
+
 extern "C" {
 
 int32_t rt_version(void) { return 100; }
@@ -463,6 +491,7 @@ rt_status rt_create(const rt_config *cfg, rt_ctx **out)
                               wavefront_uses_matrix_cores(cfg->d_model, cfg->d_hidden, c->use_mfma);
     if (rs == RT_OK && wave_prefill && !c->stack_slab && stack_workspace(c, 1, 64) != RT_OK) c->err.clear();
     if (rs == RT_OK && (cfg->reserve & RT_RESERVE_BACKWARD)) rs = ensure_backward_scratch(c);
+    if (rs == RT_OK && (cfg->reserve & RT_RESERVE_PAGED)) rs = ensure_paged_scratch(c);
     if (rs != RT_OK) {
         (void)rt_destroy(c);
         return rs;
@@ -488,6 +517,7 @@ rt_status rt_destroy(rt_ctx *c)
     group_stack_destroy(c->group_stack);
     if (c->par_slab) (void)hipFree(c->par_slab);
     if (c->bw_slab) (void)hipFree(c->bw_slab);
+    if (c->paged_slab) (void)hipFree(c->paged_slab);
     for (int g = 0; g < kMaxWaveStreams; ++g) {
         if (g > 0 && c->wave_streams.st[g]) (void)hipStreamDestroy(c->wave_streams.st[g]);
         if (c->wave_streams.ev[g]) (void)hipEventDestroy(c->wave_streams.ev[g]);
@@ -503,7 +533,7 @@ const char *rt_last_error(const rt_ctx *c) { return c ? c->err.c_str() : static_
 uint64_t rt_workspace_bytes(const rt_ctx *c)
 {
     return c ? (uint64_t)c->slab_bytes + c->kv_chunk_bytes + persistent_bytes(c->persist) + group_bytes(c->group) + c->group_f32.slab_bytes + decode_coop_bytes(c->dec) + c->stack_bytes + c->group_stack.slab_bytes +
-                   c->par_bytes + c->bw_bytes
+                   c->par_bytes + c->bw_bytes + c->paged_bytes
              : 0;
 }
 const char *rt_engine_name(const rt_ctx *c) { return c ? c->engine.c_str() : ""; }
@@ -1274,5 +1304,163 @@ extern "C" rt_status rt_layer_backward(rt_ctx *c, const rt_layer_weights *w, con
     hipError_t e = c->cfg.dtype == RT_BF16 ? backward_layer<bf16_t>(D, W, x, z, gy, gK, gV, dx, G, c->bw_slab, c->use_mfma, c->stream, &c->bw_loop)
                                            : backward_layer<float>(D, W, x, z, gy, gK, gV, dx, G, c->bw_slab, false, c->stream);
     if (e != hipSuccess) return fail_hip(c, e, "backward_layer");
+    return RT_OK;
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// Serving from pages (rt_paged.hip) and the 4-bit read-out (rt_mx4.hip).
+// ------------------------------------------------------------------------------------------------------------
+static PagedCache to_pool(const rt_paged_cache &p)
+{
+    PagedCache C;
+    C.K = p.K; C.V = p.V; C.Kx = p.K_exp; C.Vx = p.V_exp;
+    C.table = p.table; C.table_stride = p.table_stride;
+    C.pages = p.pages; C.lg = ilog2(p.page_len);
+    return C;
+}
+
+extern "C" rt_status rt_cache_write(rt_ctx *c, const rt_paged_cache *cache, int32_t S, const int32_t *first, const int32_t *count, int32_t N,
+                                    const void *k, const void *v, int64_t seq_stride, int64_t pos_stride)
+{
+    if (!c) return RT_ERR_INVALID_ARG;
+    if (c->broken) return fail(c, RT_ERR_STATE, "context is unusable after an earlier failure%s");
+    PoolRanges pool;
+    const char *msg;
+    rt_status s = check_pool(c->cfg, cache, S, &pool, &msg);
+    if (s == RT_OK) s = check_pair_rows(c->cfg, pool, first, S, N, k, v, seq_stride, pos_stride, false, &msg);
+    if (s != RT_OK) return fail(c, s, "%s", msg);
+    if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(c, RT_ERR_HIP, "hipSetDevice failed%s");
+    const PagedCache C = to_pool(*cache);
+    const PairRows R = {first, count, S, N, seq_stride, pos_stride};
+    const hipError_t e = c->cfg.dtype == RT_BF16 ? cache_write_launch<bf16_t>(C, R, c->cfg.n_heads, k, v, c->stream)
+                                                 : cache_write_launch<float>(C, R, c->cfg.n_heads, k, v, c->stream);
+    if (e != hipSuccess) return fail_hip(c, e, "cache_write");
+    return RT_OK;
+}
+
+extern "C" rt_status rt_cache_read(rt_ctx *c, const rt_paged_cache *cache, int32_t S, const int32_t *first, const int32_t *count, int32_t N,
+                                   void *k, void *v, int64_t seq_stride, int64_t pos_stride)
+{
+    if (!c) return RT_ERR_INVALID_ARG;
+    if (c->broken) return fail(c, RT_ERR_STATE, "context is unusable after an earlier failure%s");
+    PoolRanges pool;
+    const char *msg;
+    rt_status s = check_pool(c->cfg, cache, S, &pool, &msg);
+    if (s == RT_OK) s = check_pair_rows(c->cfg, pool, first, S, N, k, v, seq_stride, pos_stride, true, &msg);
+    if (s != RT_OK) return fail(c, s, "%s", msg);
+    if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(c, RT_ERR_HIP, "hipSetDevice failed%s");
+    const PagedCache C = to_pool(*cache);
+    const PairRows R = {first, count, S, N, seq_stride, pos_stride};
+    const hipError_t e = c->cfg.dtype == RT_BF16 ? cache_read_launch<bf16_t>(C, R, c->cfg.n_heads, k, v, c->stream)
+                                                 : cache_read_launch<float>(C, R, c->cfg.n_heads, k, v, c->stream);
+    if (e != hipSuccess) return fail_hip(c, e, "cache_read");
+    return RT_OK;
+}
+
+extern "C" rt_status rt_paged_attention(rt_ctx *c, const rt_paged_cache *cache, int32_t S, const int32_t *lens, int32_t max_len,
+                                        const void *q, int64_t q_stride, const void *k_t, const void *v_t, int64_t kv_stride, void *out,
+                                        int64_t out_stride, float *lse)
+{
+    if (!c) return RT_ERR_INVALID_ARG;
+    if (c->broken) return fail(c, RT_ERR_STATE, "context is unusable after an earlier failure%s");
+    PoolRanges pool;
+    const char *msg;
+    rt_status s = check_pool(c->cfg, cache, S, &pool, &msg);
+    if (s == RT_OK)
+        s = check_paged_attention(c->cfg, cache, pool, S, lens, max_len, q, q_stride, k_t, v_t, kv_stride, out, out_stride, lse, &msg);
+    if (s != RT_OK) return fail(c, s, "%s", msg);
+    if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(c, RT_ERR_HIP, "hipSetDevice failed%s");
+    if ((s = ensure_paged_scratch(c)) != RT_OK) return s;
+    PagedAttention A = {};
+    A.S = S; A.H = c->cfg.n_heads; A.max_len = max_len; A.lens = lens;
+    A.scale = c->cfg.attn_scale; A.alibi = c->cfg.alibi_max_bias;
+    A.q = q; A.kt = k_t; A.vt = v_t; A.q_stride = q_stride; A.kv_stride = kv_stride; A.out_stride = out_stride;
+    A.out = out; A.lse = lse;
+    paged_partials(A, c->paged_slab);
+    A.plan = paged_plan(max_len, S, A.H);
+    const PagedCache C = to_pool(*cache);
+    const hipError_t e = c->cfg.dtype == RT_BF16 ? paged_attention_launch<bf16_t>(C, A, c->stream) : paged_attention_launch<float>(C, A, c->stream);
+    if (e != hipSuccess) return fail_hip(c, e, "paged_attention");
+    return RT_OK;
+}
+
+template <typename T>
+static rt_status decode_paged(rt_ctx *c, LayerDims D, const rt_layer_weights *w, const PagedCache &C, const void *x_t, const int32_t *pos,
+                              int32_t max_pos, void *y_t)
+{
+    const Weights W = to_weights(w);
+    hipStream_t st = c->stream;
+    Scratch S = c->S;
+    S.Q = nullptr;   // the queries and the temporary pairs stay in fp32 rows
+    void *y_new = (char *)c->paged_slab + paged_rows_offset();
+    const bool mm = sizeof(T) == 2 && step_mm_supported(D, c->use_mfma), wide = mm && step_uses_wide(D);
+    if (wide) RT_TRY(step_qkv_wide(D, W, S, x_t, (size_t)D.d, st), "step_qkv_wide");
+    else if (mm) RT_TRY(step_qkv_mm(D, W, S, x_t, (size_t)D.d, st), "step_qkv_mm");
+    else RT_TRY(Launch<T>::qkv_raw(D, W, S, x_t, (size_t)D.d, st), "qkv_raw");
+    PagedAttention A = {};
+    A.S = D.B; A.H = D.H; A.max_len = max_pos; A.lens = pos;
+    A.scale = D.scale; A.alibi = D.alibi;
+    A.qkv = S.qkv_raw; A.g_q = W.g_q; A.g_k = W.g_k; A.normalise = !wide && !D.norm_free; A.eps = D.eps;
+    if (mm) { A.op_a = S.op_a; A.op_fragments = wide; }
+    else A.attn_cat = S.attn_cat;
+    paged_partials(A, c->paged_slab);
+    A.plan = paged_plan(max_pos, D.B, D.H);
+    RT_TRY(paged_attention_launch<T>(C, A, st), "paged_attention");
+    if (mm) {
+        RT_TRY(step_base_case_mm(D, W, S, x_t, y_new, nullptr, nullptr, st), "step_base_case_mm");
+    } else {
+        RT_TRY(Launch<T>::gemv_wo(D, W, S, x_t, (size_t)D.d, st), "gemv_wo");
+        RT_TRY(Launch<T>::gemv_w1(D, W, S, st), "gemv_w1");
+        RT_TRY(Launch<T>::gemv_w2(D, W, S, y_new, (size_t)D.d, st), "gemv_w2");
+        RT_TRY(Launch<T>::gemv_kv(D, W, S, st), "gemv_kv");
+    }
+    RT_TRY(paged_finish_launch<T>(C, D, pos, max_pos, S.kv_raw, W.g_k, !mm && !D.norm_free, y_new, y_t, st), "paged_finish");
+    return RT_OK;
+}
+
+extern "C" rt_status rt_decode_step_paged(rt_ctx *c, const rt_layer_weights *w, const rt_paged_cache *cache, const void *x_t, int32_t S,
+                                          const int32_t *pos, int32_t max_pos, void *y_t)
+{
+    if (!c) return RT_ERR_INVALID_ARG;
+    if (c->broken) return fail(c, RT_ERR_STATE, "context is unusable after an earlier failure%s");
+    rt_status s = check_weights(c, w);
+    if (s != RT_OK) return s;
+    PoolRanges pool;
+    const char *msg;
+    s = check_pool(c->cfg, cache, S, &pool, &msg);
+    if (s == RT_OK) s = check_paged_step(c->cfg, cache, pool, x_t, S, pos, max_pos, y_t, &msg);
+    if (s != RT_OK) return fail(c, s, "%s", msg);
+    if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(c, RT_ERR_HIP, "hipSetDevice failed%s");
+    if ((s = ensure_paged_scratch(c)) != RT_OK) return s;
+    LayerDims D = c->base;
+    D.B = S; D.N = 1; D.kv_cap = 1;
+    c->engine = "decode-paged";
+    c->form = kFormLaunches;
+    const PagedCache C = to_pool(*cache);
+    return c->cfg.dtype == RT_BF16 ? decode_paged<bf16_t>(c, D, w, C, x_t, pos, max_pos, y_t)
+                                   : decode_paged<float>(c, D, w, C, x_t, pos, max_pos, y_t);
+}
+
+extern "C" rt_status rt_mx4_pack(const void *W, int32_t dtype, int64_t rows, int32_t cols, uint8_t *codes, uint8_t *exps)
+{
+    if (!W || !codes || !exps || rows < 1 || cols < 1 || cols % kMx4Block != 0 || rows > ((int64_t)1 << 31)) return RT_ERR_INVALID_ARG;
+    if (dtype != RT_F32 && dtype != RT_BF16) return RT_ERR_INVALID_ARG;
+    return mx4_pack_host(W, dtype == RT_BF16, rows, cols, codes, exps) ? RT_OK : RT_ERR_INVALID_ARG;
+}
+
+extern "C" rt_status rt_lm_head_mx4(rt_ctx *c, const uint8_t *codes, const uint8_t *exps, const void *g_final, int32_t vocab, const void *z,
+                                    int64_t z_stride, int32_t B, float *logits)
+{
+    if (!c) return RT_ERR_INVALID_ARG;
+    if (c->broken) return fail(c, RT_ERR_STATE, "context is unusable after an earlier failure%s");
+    const char *msg;
+    const rt_status s = check_mx4_head(c->cfg, codes, exps, vocab, z, z_stride, B, logits, &msg);
+    if (s != RT_OK) return fail(c, s, "%s", msg);
+    if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(c, RT_ERR_HIP, "hipSetDevice failed%s");
+    const int nf = (c->cfg.flags & RT_FLAG_NORM_FREE) ? 1 : 0;
+    const hipError_t e = c->cfg.dtype == RT_BF16
+                             ? mx4_head_launch<bf16_t>(codes, exps, g_final, z, z_stride, logits, B, c->cfg.d_model, vocab, c->cfg.rms_eps, nf, c->stream)
+                             : mx4_head_launch<float>(codes, exps, g_final, z, z_stride, logits, B, c->cfg.d_model, vocab, c->cfg.rms_eps, nf, c->stream);
+    if (e != hipSuccess) return fail_hip(c, e, "lm_head_mx4");
     return RT_OK;
 }

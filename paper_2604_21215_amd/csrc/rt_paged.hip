@@ -1,0 +1,490 @@
+// Serving from pages: rows of cached pairs written (in the storage dtype or in eight bits) and read back, the attention of one new token
+// per sequence over its pages, and the end of a decoding step that caches its pair there.
+//
+// A page holds page_len positions of one sequence, head by head: [pages][H][page_len][64].  A head's run of page_len rows is contiguous
+// (2 KB and more in bf16), so a wavefront that walks one head's positions reads whole cache lines also where a row is only the 64 bytes
+// of eight bits.
+#include "rt_paged.h"
+#include "rt_ll.h"
+
+namespace rt {
+
+// ---------------------------------------------------------------- rows of 64 values, 16 bytes of them per lane
+template <typename T> constexpr int kLanesPerRow = 64 * (int)sizeof(T) / 16;   // fp32 16, bf16 8, int8 4
+template <typename T> constexpr int kPerLane = 16 / (int)sizeof(T);
+
+// sum / maximum over the lanes of a row (4, 8 or 16 neighbouring lanes: inside a row of 16 lanes, no LDS crossbar)
+template <int LPR> __device__ __forceinline__ float row_sum(float v)
+{
+    v += dpp_f(v, 0);
+    v += dpp_f(v, 1);
+    if (LPR >= 8) v += dpp_f(v, 2);
+    if (LPR >= 16) v += dpp_f(v, 3);
+    return v;
+}
+template <int LPR> __device__ __forceinline__ uint32_t row_max_bits(uint32_t v)
+{
+    v = max(v, __float_as_uint(dpp_f(__uint_as_float(v), 0)));
+    v = max(v, __float_as_uint(dpp_f(__uint_as_float(v), 1)));
+    if (LPR >= 8) v = max(v, __float_as_uint(dpp_f(__uint_as_float(v), 2)));
+    if (LPR >= 16) v = max(v, __float_as_uint(dpp_f(__uint_as_float(v), 3)));
+    return v;
+}
+
+__device__ __forceinline__ void widen(const uint4 &r, float (&f)[4], const float *)
+{
+    f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
+}
+__device__ __forceinline__ void widen(const uint4 &r, float (&f)[8], const bf16_t *)
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(w[e] << 16); f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void widen(const uint4 &r, float (&f)[16], const int8_t *)
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) f[4 * e + b] = (float)(int8_t)(w[e] >> (8 * b));
+}
+
+// fp32 -> bf16 for values that may be infinite or NaN (a NaN stays one)
+__device__ __forceinline__ bf16_t f32_to_bf16_any(float f) { return f == f ? f32_to_bf16(f) : (bf16_t)0x7FC0; }
+template <typename T> __device__ __forceinline__ T from_f32_any(float f);
+template <> __device__ __forceinline__ float from_f32_any<float>(float f) { return f; }
+template <> __device__ __forceinline__ bf16_t from_f32_any<bf16_t>(float f) { return f32_to_bf16_any(f); }
+
+// ---------------------------------------------------------------- rows into pages and back
+// The position of row n of sequence s, or -1 where there is none: an idle sequence, a row past its count.  at_end: positions that the
+// sequence's line of the table has room for.
+__device__ __forceinline__ int row_position(const PairRows &R, int s, int n, long long at_end, bool *outside)
+{
+    const int first = R.first[s];
+    const int cnt = R.count ? min(R.count[s], R.N) : R.N;
+    *outside = false;
+    if (first < 0 || n >= cnt) return -1;
+    if ((long long)first + n >= at_end) { *outside = true; return -1; }
+    return first + n;
+}
+
+// One row of one head per 4, 8 or 16 lanes, its keys and its values.  Rows of a workgroup: tiles of eight consecutive positions (one where
+// a call has fewer), head after head, so that both the 128 bytes of a head read and the runs of a page written are neighbours.
+// Bound: memory.  grid (row groups, S), block 256.
+template <typename T, bool BITS8, int TILE>
+__global__ __launch_bounds__(256) void cache_write_kernel(const PagedCache C, const PairRows R, int H, const T *__restrict__ k,
+                                                          const T *__restrict__ v)
+{
+    constexpr int LPR = kLanesPerRow<T>, PL = kPerLane<T>;
+    const int c = threadIdx.x % LPR, s = blockIdx.y;
+    const unsigned r = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;   // [tile of positions][head][position in the tile]
+    const unsigned th = r / TILE;
+    const int n = (int)(th / (unsigned)H) * TILE + (int)(r % TILE), h = (int)(th % (unsigned)H);
+    if (n >= R.N) return;
+    bool outside;
+    const int pos = row_position(R, s, n, C.table_stride << C.lg, &outside);
+    if (pos < 0) return;
+    const int page = C.table[s * C.table_stride + (pos >> C.lg)];
+    if (!page_ok(page, C.pages)) return;
+    const size_t row = pool_row(page, H, h, C.lg, pos & ((1 << C.lg) - 1));
+    const long long src = s * R.seq_stride + n * R.pos_stride + h * kHeadDim + c * PL;
+    const uint4 kr = *reinterpret_cast<const uint4 *>(k + src), vr = *reinterpret_cast<const uint4 *>(v + src);
+    if (!BITS8) {
+        *reinterpret_cast<uint4 *>((T *)C.K + row * kHeadDim + c * PL) = kr;
+        *reinterpret_cast<uint4 *>((T *)C.V + row * kHeadDim + c * PL) = vr;
+        return;
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        float f[PL];
+        widen(w ? vr : kr, f, (const T *)nullptr);
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < PL; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+        const int byte = row_exponent(row_max_bits<LPR>(top));
+        const float inv = __uint_as_float(exponent_inverse_bits(byte));
+        uint32_t packed[PL / 4];
+#pragma unroll
+        for (int e = 0; e < PL; ++e) {
+            const int code = byte == 255 ? 0 : (int)rintf(f[e] * inv);
+            if (e % 4 == 0) packed[e / 4] = 0;
+            packed[e / 4] |= (uint32_t)(code & 255) << (8 * (e % 4));
+        }
+        uint32_t *dst = reinterpret_cast<uint32_t *>((int8_t *)(w ? C.V : C.K) + row * kHeadDim + c * PL);
+#pragma unroll
+        for (int e = 0; e < PL / 4; ++e) dst[e] = packed[e];
+        if (c == 0) (w ? C.Vx : C.Kx)[row] = (uint8_t)byte;
+    }
+}
+
+template <typename T, bool BITS8, int TILE>
+__global__ __launch_bounds__(256) void cache_read_kernel(const PagedCache C, const PairRows R, int H, T *__restrict__ k,
+                                                         T *__restrict__ v)
+{
+    constexpr int LPR = kLanesPerRow<T>, PL = kPerLane<T>;
+    const int c = threadIdx.x % LPR, s = blockIdx.y;
+    const unsigned r = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, th = r / TILE;
+    const int n = (int)(th / (unsigned)H) * TILE + (int)(r % TILE), h = (int)(th % (unsigned)H);
+    if (n >= R.N) return;
+    bool outside;
+    const int pos = row_position(R, s, n, C.table_stride << C.lg, &outside);
+    if (pos < 0 && !outside) return;
+    const int page = outside ? -1 : C.table[s * C.table_stride + (pos >> C.lg)];
+    const bool ok = page_ok(page, C.pages);   // no such page: the row reads as NaN
+    const size_t row = ok ? pool_row(page, H, h, C.lg, pos & ((1 << C.lg) - 1)) : 0;
+    const long long dst = s * R.seq_stride + n * R.pos_stride + h * kHeadDim + c * PL;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        float f[PL];
+        uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+        if (!BITS8) {
+            if (ok) raw = *reinterpret_cast<const uint4 *>((const T *)(w ? C.V : C.K) + row * kHeadDim + c * PL);
+            else if (sizeof(T) == 4) raw = make_uint4(0x7FC00000u, 0x7FC00000u, 0x7FC00000u, 0x7FC00000u);
+            else raw = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
+            *reinterpret_cast<uint4 *>((w ? v : k) + dst) = raw;
+            continue;
+        }
+        const float step = __uint_as_float(exponent_step_bits(ok ? (w ? C.Vx : C.Kx)[row] : 255));
+        const uint32_t *src = reinterpret_cast<const uint32_t *>((const int8_t *)(w ? C.V : C.K) + row * kHeadDim + c * PL);
+#pragma unroll
+        for (int e = 0; e < PL / 4; ++e) {
+            const uint32_t u = src[e];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) f[4 * e + b] = (float)(int8_t)(u >> (8 * b)) * step;
+        }
+        T o[PL];
+#pragma unroll
+        for (int e = 0; e < PL; ++e) o[e] = from_f32_any<T>(f[e]);   // exact: codes have seven bits
+        __builtin_memcpy(&raw, o, 16);
+        *reinterpret_cast<uint4 *>((w ? v : k) + dst) = raw;
+    }
+}
+
+template <typename T, int TILE> static dim3 rows_grid(const PairRows &R, int H)
+{
+    const long long rows = (long long)((R.N + TILE - 1) / TILE) * TILE * H, per = 256 / kLanesPerRow<T>;
+    return dim3((unsigned)((rows + per - 1) / per), (unsigned)R.S);
+}
+template <typename T, int TILE> static void cache_write_go(const PagedCache &C, const PairRows &R, int H, const T *k, const T *v, hipStream_t st)
+{
+    const dim3 grid = rows_grid<T, TILE>(R, H);
+    if (C.Kx) hipLaunchKernelGGL((cache_write_kernel<T, true, TILE>), grid, dim3(256), 0, st, C, R, H, k, v);
+    else hipLaunchKernelGGL((cache_write_kernel<T, false, TILE>), grid, dim3(256), 0, st, C, R, H, k, v);
+}
+template <typename T, int TILE> static void cache_read_go(const PagedCache &C, const PairRows &R, int H, T *k, T *v, hipStream_t st)
+{
+    const dim3 grid = rows_grid<T, TILE>(R, H);
+    if (C.Kx) hipLaunchKernelGGL((cache_read_kernel<T, true, TILE>), grid, dim3(256), 0, st, C, R, H, k, v);
+    else hipLaunchKernelGGL((cache_read_kernel<T, false, TILE>), grid, dim3(256), 0, st, C, R, H, k, v);
+}
+template <typename T> hipError_t cache_write_launch(const PagedCache &C, const PairRows &R, int H, const void *k, const void *v, hipStream_t st)
+{
+    if (R.N >= 8) cache_write_go<T, 8>(C, R, H, (const T *)k, (const T *)v, st);
+    else cache_write_go<T, 1>(C, R, H, (const T *)k, (const T *)v, st);
+    return hipGetLastError();
+}
+template <typename T> hipError_t cache_read_launch(const PagedCache &C, const PairRows &R, int H, void *k, void *v, hipStream_t st)
+{
+    if (R.N >= 8) cache_read_go<T, 8>(C, R, H, (T *)k, (T *)v, st);
+    else cache_read_go<T, 1>(C, R, H, (T *)k, (T *)v, st);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- attention of one new token
+// out = sum_j softmax_j(scale <q, k_j> - slope (n - j)) v_j over the n cached rows and the pair of the token itself (distance 0).
+// One pass with a running maximum and sum, kept per group of lanes that shares a row (4, 8 or 16 of them): nothing crosses the groups
+// inside the loop.  The running maximum starts at the lowest finite number, so an empty row needs no special case: its sum is 0.
+constexpr float kLowest = -3.402823466e38f;
+__device__ __forceinline__ float exp_diff(float a, float m) { return __expf(a - m); }
+
+// q and the pair of (s, h) as 64 values, one per lane
+template <typename T, bool STEP> struct TokenRows {
+    float q, kt, vt;
+    bool pair;
+    __device__ __forceinline__ TokenRows(const PagedAttention &A, int s, int h)
+    {
+        const int lane = threadIdx.x & 63;
+        if (STEP) {
+            const int d = A.H * kHeadDim;
+            const float *r = A.qkv + (size_t)s * 3 * d + h * kHeadDim + lane;
+            q = r[0]; kt = r[d]; vt = r[2 * d];
+            pair = true;
+            if (A.normalise) {
+                q = head_norm(q, (const T *)A.g_q, h, A.eps);
+                kt = head_norm(kt, (const T *)A.g_k, h, A.eps);
+            }
+        } else {
+            q = to_f32(((const T *)A.q)[s * A.q_stride + h * kHeadDim + lane]);
+            pair = A.kt != nullptr;
+            kt = pair ? to_f32(((const T *)A.kt)[s * A.kv_stride + h * kHeadDim + lane]) : 0.f;
+            vt = pair ? to_f32(((const T *)A.vt)[s * A.kv_stride + h * kHeadDim + lane]) : 0.f;
+        }
+    }
+    static __device__ __forceinline__ float head_norm(float v, const T *g, int h, float eps)
+    {
+        return v * rsqrtf(fast_sum(v * v) / (float)kHeadDim + eps) * (g ? to_f32(g[h * kHeadDim + (threadIdx.x & 63)]) : 1.f);
+    }
+};
+
+// The finished row of (s, h): lane = dimension, (m, l, o) the state over the cached rows; bad: NaN.
+template <typename T, bool STEP>
+__device__ __forceinline__ void finish_row(const PagedAttention &A, int s, int h, const TokenRows<T, STEP> &t, float m, float l, float o, bool bad)
+{
+    const int lane = threadIdx.x & 63;
+    if (t.pair) {
+        const float z = A.scale * fast_sum(t.q * t.kt), mx = fmaxf(m, z);
+        const float e0 = exp_diff(m, mx), e1 = exp_diff(z, mx);
+        l = fmaf(l, e0, e1);
+        o = fmaf(o, e0, e1 * t.vt);
+        m = mx;
+    }
+    float a = l == 0.f ? 0.f : o / l;
+    if (bad) a = __uint_as_float(0x7FC00000u);
+    if (STEP) {
+        const int d = A.H * kHeadDim;
+        if (A.attn_cat) A.attn_cat[(size_t)s * d + h * kHeadDim + lane] = a;
+        if (A.op_a) {
+            const bf16_t hi = f32_to_bf16_any(a);
+            const ulonglong2 oo = operand_offsets(A.op_fragments != 0, A.S, d, s, h * kHeadDim + lane);
+            A.op_a[oo.x] = hi;
+            A.op_a[oo.y] = f32_to_bf16_any(a - bf16_to_f32(hi));
+        }
+    } else {
+        ((T *)A.out)[s * A.out_stride + h * kHeadDim + lane] = from_f32_any<T>(a);
+        if (A.lse && lane == 0) A.lse[(size_t)s * A.H + h] = bad ? __uint_as_float(0x7FC00000u) : (l == 0.f ? -INFINITY : m + logf(l));
+    }
+}
+
+// C: type of the cached values (T or int8_t).  Workgroup = (split, h, s), its four wavefronts share the split's rows in four runs.
+// A wavefront loads NL times 64 / LPR rows of keys and of values before it computes on them.
+template <typename T, typename C, bool STEP>
+__global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P, const PagedAttention A)
+{
+    constexpr int LPR = kLanesPerRow<C>, PL = kPerLane<C>, RPL = 64 / LPR, NL = sizeof(C) == 1 ? 4 : 8, CH = NL * RPL;
+    constexpr bool Q8 = sizeof(C) == 1;
+    __shared__ float sm[4 * RPL], sl[4 * RPL];
+    __shared__ float so[4 * RPL][kHeadDim];
+    __shared__ int sbad[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int split = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+    const int n = A.lens[s];
+    const int lo = split * A.plan.split_len;
+    const bool one = A.plan.n_splits == 1;
+    if (n < 0 || n > A.max_len) {
+        if (split == 0 && wave == 0 && (STEP || n > 0)) {   // an idle row of a step: zeros for the products; too long: NaN
+            TokenRows<T, STEP> t(A, s, h);
+            t.pair = false;
+            finish_row<T, STEP>(A, s, h, t, kLowest, 0.f, 0.f, n > 0);
+        }
+        return;
+    }
+    if (lo >= n && !one) return;   // no rows here; the join counts the splits in the same way
+    const int hi = min(n, lo + A.plan.split_len);
+    // this wavefront's run: a quarter of the rows in whole chunks
+    const int share = ((hi - lo + 4 * CH - 1) / (4 * CH)) * CH;
+    const int wlo = lo + wave * share, whi = min(hi, wlo + share);
+
+    const int c = lane % LPR, g = lane / LPR;
+    TokenRows<T, STEP> tok(A, s, h);
+    float q[PL];
+#pragma unroll
+    for (int e = 0; e < PL; ++e) q[e] = __shfl(tok.q, c * PL + e, 64);
+    float m = kLowest, l = 0.f, o[PL];
+#pragma unroll
+    for (int e = 0; e < PL; ++e) o[e] = 0.f;
+    const float slope = alibi_slope(A.alibi, h, A.H);
+    bool bad = false;
+    const int last_page = (n - 1) >> P.lg;
+    const int32_t *line = P.table + s * P.table_stride;
+    int base = 0, entry = 0, have = 0;   // lane i holds the entry of page base + i of the sequence, i < have
+    for (int r0 = wlo; r0 < whi; r0 += CH) {
+        if (((r0 + CH - 1) >> P.lg) >= base + have) {
+            base = r0 >> P.lg;
+            have = 64;
+            const int p = min(base + lane, last_page);
+            entry = line[p];
+            const bool wrong = !page_ok(entry, P.pages);
+            if (wrong) entry = 0;
+            bad = bad || __any(wrong && ((base + lane) << P.lg) < whi);
+        }
+        uint4 kr[NL], vr[NL];
+        float ks[NL], vs[NL];
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int r = r0 + i * RPL;
+            const int page = __builtin_amdgcn_readlane(entry, min(r >> P.lg, last_page) - base);
+            const size_t row = pool_row(page, A.H, h, P.lg, r & ((1 << P.lg) - 1)) + g;
+            kr[i] = *reinterpret_cast<const uint4 *>((const C *)P.K + row * kHeadDim + c * PL);
+            vr[i] = *reinterpret_cast<const uint4 *>((const C *)P.V + row * kHeadDim + c * PL);
+            if (Q8) {
+                ks[i] = __uint_as_float(exponent_step_bits(P.Kx[row]));
+                vs[i] = __uint_as_float(exponent_step_bits(P.Vx[row]));
+            }
+        }
+        float z[NL], mx = m;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            float f[PL], acc = 0.f;
+            widen(kr[i], f, (const C *)nullptr);
+#pragma unroll
+            for (int e = 0; e < PL; ++e) acc = fmaf(q[e], f[e], acc);
+            acc = row_sum<LPR>(acc) * A.scale;
+            if (Q8) acc *= ks[i];
+            const int r = r0 + i * RPL + g;
+            z[i] = r < whi ? fmaf(-slope, (float)(n - r), acc) : -INFINITY;
+            mx = fmaxf(mx, z[i]);
+        }
+        const float f0 = exp_diff(m, mx);
+        l *= f0;
+#pragma unroll
+        for (int e = 0; e < PL; ++e) o[e] *= f0;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const float p = exp_diff(z[i], mx);
+            l += p;
+            float f[PL];
+            widen(vr[i], f, (const C *)nullptr);
+            const bool in = r0 + i * RPL + g < whi;   // what lies behind the last row may be anything
+            const float w = Q8 ? (in ? p * vs[i] : 0.f) : p;
+#pragma unroll
+            for (int e = 0; e < PL; ++e) o[e] = fmaf(w, Q8 || in ? f[e] : 0.f, o[e]);
+        }
+        m = mx;
+    }
+    // the groups' states meet in LDS
+    const int grp = wave * RPL + g;
+    if (c == 0) { sm[grp] = m; sl[grp] = l; }
+    if (lane == 0) sbad[wave] = bad;
+    __syncthreads();
+    float M = kLowest;
+    if (lane < 4 * RPL) M = sm[lane];
+    M = fast_max(M);
+    const float wgt = exp_diff(m, M);
+#pragma unroll
+    for (int e = 0; e < PL; ++e) so[grp][c * PL + e] = o[e] * wgt;
+    __syncthreads();
+    if (wave != 0) return;
+    float L = lane < 4 * RPL ? sl[lane] * exp_diff(sm[lane], M) : 0.f;
+    L = fast_sum(L);
+    float O = 0.f;
+    for (int i = 0; i < 4 * RPL; ++i) O += so[i][lane];
+    const bool any_bad = sbad[0] | sbad[1] | sbad[2] | sbad[3];
+    if (one) {
+        finish_row<T, STEP>(A, s, h, tok, M, L, O, any_bad);
+        return;
+    }
+    if (any_bad) L = __uint_as_float(0x7FC00000u);
+    const size_t idx = ((size_t)s * A.H + h) * A.plan.n_splits + split;
+    if (lane == 0) { A.pm[idx] = M; A.pl[idx] = L; }
+    A.po[idx * kHeadDim + lane] = O;
+}
+
+// The splits of every (s, h) joined, one wavefront each: the largest maximum first, then the weighted sums in split order.
+// grid ceil(S H / 4), block 256.
+template <typename T, bool STEP> __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttention A)
+{
+    const int lane = threadIdx.x & 63, sh = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (sh >= A.S * A.H) return;
+    const int s = sh / A.H, h = sh % A.H;
+    const int n = A.lens[s];
+    if (n < 0 || n > A.max_len) return;   // done by the splits' launch
+    const int ns = (n + A.plan.split_len - 1) / A.plan.split_len;
+    const float *pm = A.pm + (size_t)sh * A.plan.n_splits, *pl = A.pl + (size_t)sh * A.plan.n_splits;
+    const float *po = A.po + (size_t)sh * A.plan.n_splits * kHeadDim + lane;
+    TokenRows<T, STEP> tok(A, s, h);
+    float m = kLowest, l = 0.f, o = 0.f;
+    for (int i = lane; i < ns; i += 64) m = fmaxf(m, pm[i]);
+    m = fast_max(m);
+    for (int i0 = 0; i0 < ns; i0 += 64) {
+        const int i = i0 + lane, cnt = min(64, ns - i0);
+        const float w = i < ns ? exp_diff(pm[i], m) : 0.f;
+        const float lw = i < ns ? w * pl[i] : 0.f;
+        l += fast_sum(lw);
+        for (int j0 = 0; j0 < cnt; j0 += 8) {   // eight state rows in flight
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = po[(size_t)(i0 + min(j0 + e, cnt - 1)) * kHeadDim];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o = fmaf(j0 + e < cnt ? lane_bcast(w, min(j0 + e, 63)) : 0.f, v[e], o);
+        }
+    }
+    finish_row<T, STEP>(A, s, h, tok, m, l, o, false);
+}
+
+SplitPlan paged_plan(int max_len, int S, int H) { return split_plan(max_len, S, H, 2048, 1024); }
+size_t paged_partials_bytes() { return (size_t)kMaxPartials * (kHeadDim + 2) * 4; }
+void paged_partials(PagedAttention &A, void *slab)
+{
+    A.po = (float *)slab;
+    A.pm = A.po + (size_t)kMaxPartials * kHeadDim;
+    A.pl = A.pm + kMaxPartials;
+}
+
+template <typename T, bool STEP> static hipError_t attention_launch(const PagedCache &C, const PagedAttention &A, hipStream_t st)
+{
+    const dim3 grid((unsigned)A.plan.n_splits, (unsigned)A.H, (unsigned)A.S);
+    if (C.Kx) hipLaunchKernelGGL((paged_attention_kernel<T, int8_t, STEP>), grid, dim3(256), 0, st, C, A);
+    else hipLaunchKernelGGL((paged_attention_kernel<T, T, STEP>), grid, dim3(256), 0, st, C, A);
+    if (A.plan.n_splits > 1)
+        hipLaunchKernelGGL((paged_join_kernel<T, STEP>), dim3((unsigned)((A.S * A.H + 3) / 4)), dim3(256), 0, st, A);
+    return hipGetLastError();
+}
+template <typename T> hipError_t paged_attention_launch(const PagedCache &C, const PagedAttention &A, hipStream_t st)
+{
+    return A.qkv ? attention_launch<T, true>(C, A, st) : attention_launch<T, false>(C, A, st);
+}
+
+// ---------------------------------------------------------------- the end of a paged step
+// One wavefront per (s, h): qkRMS of the key if it is still to be taken, the pair into its page row (rounded once from fp32, to the
+// storage dtype or to codes), and the head's slice of y.  grid (H, S), block 64.
+template <typename T>
+__global__ __launch_bounds__(64) void paged_finish_kernel(const PagedCache C, const int32_t *__restrict__ pos_of, int max_pos,
+                                                          const float *__restrict__ kv, const T *__restrict__ g_k, int normalise, int H,
+                                                          float eps, const T *__restrict__ y_new, T *__restrict__ y)
+{
+    const int lane = threadIdx.x, h = blockIdx.x, s = blockIdx.y, d = H * kHeadDim;
+    const int pos = pos_of[s];
+    if (pos < 0) return;
+    const size_t yo = (size_t)s * d + h * kHeadDim + lane;
+    y[yo] = y_new[yo];
+    if (pos > max_pos) return;
+    const int page = C.table[s * C.table_stride + (pos >> C.lg)];
+    if (!page_ok(page, C.pages)) return;
+    const size_t row = pool_row(page, H, h, C.lg, pos & ((1 << C.lg) - 1));
+    float k = kv[(size_t)s * 2 * d + h * kHeadDim + lane];
+    const float v = kv[(size_t)s * 2 * d + d + h * kHeadDim + lane];
+    if (normalise) k = TokenRows<T, true>::head_norm(k, g_k, h, eps);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const float u = w ? v : k;
+        if (!C.Kx) { ((T *)(w ? C.V : C.K))[row * kHeadDim + lane] = from_f32_any<T>(u); continue; }
+        uint32_t top = __float_as_uint(u) & 0x7FFFFFFFu;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+        const int byte = row_exponent(top);
+        const int code = byte == 255 ? 0 : (int)rintf(u * __uint_as_float(exponent_inverse_bits(byte)));
+        ((int8_t *)(w ? C.V : C.K))[row * kHeadDim + lane] = (int8_t)code;
+        if (lane == 0) (w ? C.Vx : C.Kx)[row] = (uint8_t)byte;
+    }
+}
+template <typename T>
+hipError_t paged_finish_launch(const PagedCache &C, const LayerDims &D, const int32_t *pos, int max_pos, const float *kv, const void *g_k,
+                               bool normalise, const void *y_new, void *y, hipStream_t st)
+{
+    hipLaunchKernelGGL(paged_finish_kernel<T>, dim3((unsigned)D.H, (unsigned)D.B), dim3(64), 0, st, C, pos, max_pos, kv, (const T *)g_k,
+                       normalise ? 1 : 0, D.H, D.eps, (const T *)y_new, (T *)y);
+    return hipGetLastError();
+}
+
+#define RT_PAGED_FOR(T)                                                                                                          \
+    template hipError_t cache_write_launch<T>(const PagedCache &, const PairRows &, int, const void *, const void *, hipStream_t); \
+    template hipError_t cache_read_launch<T>(const PagedCache &, const PairRows &, int, void *, void *, hipStream_t);            \
+    template hipError_t paged_attention_launch<T>(const PagedCache &, const PagedAttention &, hipStream_t);                      \
+    template hipError_t paged_finish_launch<T>(const PagedCache &, const LayerDims &, const int32_t *, int, const float *,       \
+                                               const void *, bool, const void *, void *, hipStream_t);
+RT_PAGED_FOR(float)
+RT_PAGED_FOR(bf16_t)
+#undef RT_PAGED_FOR
+
+}  // namespace rt

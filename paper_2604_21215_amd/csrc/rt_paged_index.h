@@ -1,0 +1,65 @@
+// Arithmetic of the paged cache that is the same on the host and on the device (plain C++, no HIP types): where a row lies,
+// which exponent an 8-bit row takes, and how a call's positions are cut into splits.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#if defined(__HIPCC__)
+#define RT_BOTH __host__ __device__ __forceinline__
+#else
+#define RT_BOTH inline
+#endif
+
+namespace rt {
+
+constexpr int kMinPage = 16, kMaxPage = 1024;   // positions of a page: a power of two in this range
+
+// Row (of 64 values) of position j of a page, head h, in a pool [pages][H][page_len][64] with page_len = 2^lg.
+RT_BOTH size_t pool_row(int page, int H, int h, int lg, int j) { return ((((size_t)page * (size_t)H) + (size_t)h) << lg) + (size_t)j; }
+
+// A page table's entry is used only if it names a page of the pool.
+RT_BOTH bool page_ok(int entry, int pages) { return (uint32_t)entry < (uint32_t)pages; }
+
+// 8-bit rows: the values u of a row are held as codes rint(u 2^-e), |code| <= 127, with the smallest e >= -126 for which
+// max |u| <= 127 2^e, and the byte e + 127.  Steps are powers of two: u 2^-e and code 2^e are exact, so a code never depends on how a
+// quotient was rounded, and what is read back is exact in bf16 as well (seven bits).  Byte 0: all values are 0.  Byte 255: a value of
+// the row is not finite; the row reads as NaN.
+// top: the largest of the row's values as bits, sign cleared (as integers these order like the values, NaN above all).
+RT_BOTH int row_exponent(uint32_t top)
+{
+    const int E = (int)(top >> 23);
+    if (E == 255) return 255;
+    if (top == 0) return 0;
+    // top = 1.m 2^(E-127): 1.m 2^6 <= 127 holds up to m = 0x7E0000
+    const int byte = E - 6 + ((top & 0x7FFFFFu) > 0x7E0000u ? 1 : 0);
+    return byte < 1 ? 1 : byte;
+}
+RT_BOTH uint32_t exponent_step_bits(int byte) { return byte == 255 ? 0x7FC00000u : (uint32_t)byte << 23; }          // 2^e, 0 or NaN
+RT_BOTH uint32_t exponent_inverse_bits(int byte) { return byte == 0 || byte == 255 ? 0u : (uint32_t)(254 - byte) << 23; }   // 2^-e, or 0
+
+// How the positions below max_len of S sequences and H heads are cut: workgroups of split_len positions each (the last one shorter).
+struct SplitPlan {
+    int split_len, n_splits;
+};
+constexpr int kMaxPartials = 65536;    // stored partial states of a call: S * H * n_splits if n_splits > 1
+constexpr int kSplitUnit = 256;        // four wavefronts of 64 positions
+RT_BOTH SplitPlan split_plan(int max_len, int S, int H, int want_groups, int longest)
+{
+    const int64_t pairs = (int64_t)S * H;
+    int64_t want = (want_groups + pairs - 1) / pairs;                 // splits that fill the chip
+    const int64_t least = ((int64_t)max_len + longest - 1) / longest;  // splits that keep the longest sequence's share short
+    if (want < least) want = least;
+    const int64_t most = kMaxPartials / pairs;
+    if (want > most) want = most;
+    if (want < 1) want = 1;
+    int64_t len = ((int64_t)max_len + want - 1) / want;
+    len = (len + kSplitUnit - 1) / kSplitUnit * kSplitUnit;
+    if (len < kSplitUnit) len = kSplitUnit;
+    SplitPlan p;
+    p.split_len = (int)len;
+    p.n_splits = (int)(((int64_t)max_len + len - 1) / len);
+    if (p.n_splits < 1) p.n_splits = 1;
+    return p;
+}
+
+}  // namespace rt

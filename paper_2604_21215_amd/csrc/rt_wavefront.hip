@@ -243,6 +243,12 @@ __device__ __forceinline__ void mm_epilogue(const WaveLayer &Y, int t, const f32
             for (int r = 0; r < 4; ++r) v[r] *= sc * (gn ? bf16_to_f32(gn[h * kHeadDim + hd + r]) : 1.f);
         }
         void *q = in_register(Y.S.Q), *k = in_register(Y.S.Kt), *vv = in_register(Y.S.Vt);
+        if (!q) {   // the rows in fp32 (a step from pages)
+            if (live)
+                *reinterpret_cast<float4 *>(Y.S.qkv_raw + (size_t)b * 3 * d + (size_t)which * d + h * kHeadDim + hd) =
+                    make_float4(v[0], v[1], v[2], v[3]);
+            return;
+        }
         if (live)
             *reinterpret_cast<uint2 *>((bf16_t *)(which == 0 ? q : (which == 1 ? k : vv)) + ((size_t)b * H + h) * kHeadDim + hd) =
                 make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
@@ -255,6 +261,11 @@ __device__ __forceinline__ void mm_epilogue(const WaveLayer &Y, int t, const f32
             const bf16_t *gk = (const bf16_t *)Y.W.g_k;
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] *= sc * (gk ? bf16_to_f32(gk[hh * kHeadDim + 16 * rg + 4 * g + r]) : 1.f);
+        }
+        if (!Y.K) {   // the pair in fp32 rows [k | v] (a step from pages)
+            if (live)
+                *reinterpret_cast<float4 *>(Y.S.kv_raw + (size_t)b * 2 * d + hh * kHeadDim + 16 * rg + 4 * g) = make_float4(v[0], v[1], v[2], v[3]);
+            return;
         }
         if (live) {
             const int h = is_k ? hh : hh - H, bh = b * H + h, BH = B * H;
@@ -1036,7 +1047,7 @@ static WaveLayer step_layer(const Weights &W, const Scratch &S, const void *x_t,
 
 bool step_uses_wide(const LayerDims &D) { return D.B >= kWideFrom && D.d >= kWideWidth; }
 
-// Q, Kt, Vt of the rows x_t [B][d] (step_uses_wide)
+// Q, Kt, Vt of the rows x_t [B][d] (step_uses_wide); S.Q null: in fp32, normalised, into S.qkv_raw
 hipError_t step_qkv_wide(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, size_t x_stride, hipStream_t st)
 {
     if (x_stride != (size_t)D.d) return hipErrorInvalidValue;   // Wo's epilogue addresses the rows of x_t d apart
@@ -1058,7 +1069,8 @@ hipError_t step_qkv_mm(const LayerDims &D, const Weights &W, const Scratch &S, c
     return step_mm_launch<EPI_QKV, 4, 4>(Y, 3 * D.d, D, st);
 }
 
-// h = x_t + alpha Wo a (a as operand rows in S.op_a), MLP, y_t, and the persistent pair into K_row, V_row ([B][H][64])
+// h = x_t + alpha Wo a (a as operand rows in S.op_a), MLP, y_t, and the persistent pair into K_row, V_row ([B][H][64]);
+// K_row null: in fp32 into S.kv_raw
 hipError_t step_base_case_mm(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, void *y_t, void *K_row,
                              void *V_row, hipStream_t st)
 {
