@@ -351,7 +351,7 @@ rt_status rt_mx4_pack(const void *W, int32_t dtype, int64_t rows, int32_t cols, 
 
 /* rt_lm_head with such a matrix: logits[b, v] = < W4[v, :], RMS(z_b; g_final) >, fp32 accuracy for the weights as they are packed.
  *   codes [vocab][d / 2] (on 16 bytes), exps [vocab][d / 32] device; a scale byte of 0 or 255 makes its row's logits NaN,
- *   a weight past fp32's range counts as infinite.  Other arguments
+ *   a weight past fp32's range makes them infinite or NaN.  Other arguments
  *   as rt_lm_head; d_model <= 25856; logits must not overlap an input. */
 rt_status rt_lm_head_mx4(rt_ctx *ctx, const uint8_t *codes, const uint8_t *exps, const void *g_final, int32_t vocab, const void *z,
                          int64_t z_stride, int32_t B, float *logits);

@@ -191,23 +191,29 @@ def make_weights(w: dict) -> rt_layer_weights:
 
 def make_cache(K, V, table, K_exp=None, V_exp=None) -> rt_paged_cache:
     """K, V [pages, H, page_len, 64] (storage dtype, or int8 with the bytes K_exp, V_exp [pages, H, page_len]), table int32 [S, entries]."""
-    for t in (K, V, K_exp, V_exp):
-        if t is not None and not t.is_contiguous():
-            raise RTError("RT_ERR_INVALID_ARG", "the arrays of a cache are contiguous")
-    if K.shape != V.shape or K.dim() != 4 or K.dtype != V.dtype or any(e is not None and e.shape != K.shape[:3] for e in (K_exp, V_exp)):
-        raise RTError("RT_ERR_INVALID_ARG", "K, V [pages, H, page_len, 64] and, in 8 bits, K_exp, V_exp [pages, H, page_len]")
-    if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1) or table.element_size() != 4:
+    shape = K.shape
+    if not (K.is_contiguous() and V.is_contiguous()) or V.shape != shape or len(shape) != 4 or K.dtype != V.dtype:
+        raise RTError("RT_ERR_INVALID_ARG", "K, V are contiguous [pages, H, page_len, 64] of one type")
+    ke = ve = None
+    if K_exp is not None:
+        if V_exp is None or K_exp.shape != shape[:3] or V_exp.shape != shape[:3] or not (K_exp.is_contiguous() and V_exp.is_contiguous()):
+            raise RTError("RT_ERR_INVALID_ARG", "K_exp, V_exp are contiguous [pages, H, page_len]")
+        ke, ve = K_exp.data_ptr(), V_exp.data_ptr()
+    rows, entries = table.shape
+    if table.element_size() != 4 or (entries > 1 and table.stride(1) != 1):
         raise RTError("RT_ERR_INVALID_ARG", "table is int32 [S, entries]")
-    return rt_paged_cache(K.data_ptr(), V.data_ptr(), None if K_exp is None else K_exp.data_ptr(), None if V_exp is None else V_exp.data_ptr(),
-                          table.data_ptr(), table.stride(0) if table.shape[0] > 1 else table.shape[1], K.shape[0], K.shape[2],
+    return rt_paged_cache(K.data_ptr(), V.data_ptr(), ke, ve, table.data_ptr(), table.stride(0) if rows > 1 else entries, shape[0], shape[2],
                           8 if K.element_size() == 1 else 0)
 
 
 def _pair_strides(k, v):
     """k, v [S, N, H, 64] with the same strides and the last two dimensions contiguous -> (seq_stride, pos_stride)."""
-    S, N, H, dh = k.shape
+    shape, stride = k.shape, k.stride()
+    if v.shape == shape and v.stride() == stride and stride[3] == 1 and stride[2] == shape[3]:
+        return stride[:2]
+    S, N, H, dh = shape   # dimensions of one row have no stride
     strides = lambda t: (t.stride(0) if S > 1 else 0, t.stride(1) if N > 1 else 0, t.stride(2) if H > 1 else dh, t.stride(3))  # noqa: E731
-    if v.shape != k.shape or strides(v) != strides(k) or strides(k)[2:] != (dh, 1):
+    if v.shape != shape or strides(v) != strides(k) or strides(k)[2:] != (dh, 1):
         raise RTError("RT_ERR_INVALID_ARG", "k and v are [S, N, H, 64] with equal strides and contiguous heads")
     return strides(k)[:2]
 

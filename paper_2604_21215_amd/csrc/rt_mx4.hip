@@ -1,7 +1,7 @@
 // The read-out of a stack with 4-bit weights: blocks of 32 weights of a row share a scale 2^e, a weight is a sign and one of
 // 0, 1/2, 1, 3/2, 2, 3, 4, 6 (the MX format with 4-bit elements, E2M1 codes and E8M0 scales): 17 bytes for 32 weights.
 #include "rt_mx4.h"
-#include "rt_mfma_device.h"
+#include "rt_ll.h"
 
 #include <cmath>
 
@@ -69,16 +69,12 @@ bool mx4_pack_host(const void *W, bool bf16, long long rows, int cols, uint8_t *
 
 // ---------------------------------------------------------------- logits (device)
 // logits[b][v] = sum_k W[v][k] n_b[k], n_b = g z_b / rms(z_b): D[16 vocabulary rows][16 batch columns] += W[16][32] n^T[32][16].
-// The weights are exact in bf16 (two bits and a power of two) and one instruction turns two codes into two bf16 with their scale; the rows
-// n_b are staged as three bf16 parts whose sum holds all 24 bits, so the logits carry fp32 accuracy: every weight fragment feeds three
-// matrix instructions.  A lane holds one whole block of a row: its 16 bytes of codes are four fragments, and the contraction index is dealt
-// so that slot 8 g + e of instruction j is k = 32 (4 step + g) + 8 j + e for lane group g.
-// grid (<= row tiles / 4, batch tiles of bt), block 256, LDS 3 bt ld bf16.
+// The weights are exact in bf16 (two bits and a power of two), and one instruction turns two codes into two bf16 with their scale.  A lane
+// holds one whole block of a row: its 16 bytes of codes are four fragments, and the contraction index is dealt so that slot 8 g + e of
+// instruction j is k = 128 slice + 32 g + 8 j + e for lane group g.
+// The rows must not lose what fp32 logits hold, so an element enters as bf16 parts that add up to all of it: one part for bf16 rows without a
+// gain, two for bf16 rows with one (a product of two eight-bit significands has sixteen), three for fp32.
 typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
-constexpr size_t kMxMaxLds = 152 * 1024;
-
-__host__ __device__ static inline int mx_ld(int d) { return (d + 127) / 128 * 128 + 8; }   // a row's elements in LDS
-static_assert(3 * ((kMx4MaxWidth + 127) / 128 * 128 + 8) * 2 <= kMxMaxLds, "the widest row");
 
 template <int BYTE> __device__ __forceinline__ uint32_t two_weights(uint32_t codes, float scale)
 {
@@ -86,8 +82,214 @@ template <int BYTE> __device__ __forceinline__ uint32_t two_weights(uint32_t cod
     return __builtin_bit_cast(uint32_t, r);
 }
 
+__device__ __forceinline__ Frag weight_fragment(uint32_t codes, float scale)
+{
+    Frag f;
+    f.u = make_uint4(two_weights<0>(codes, scale), two_weights<1>(codes, scale), two_weights<2>(codes, scale), two_weights<3>(codes, scale));
+    return f;
+}
+
+// v as the sum of PARTS bf16 values, by truncation: a value beyond the largest bf16 has a finite head then, and every difference is exact
+template <int PARTS> __device__ __forceinline__ void split_parts(float v, uint32_t (&p)[PARTS])
+{
+    float r = v;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        p[i] = __float_as_uint(r) & 0xFFFF0000u;
+        r = (p[i] & 0x7F800000u) == 0x7F800000u ? 0.f : r - __uint_as_float(p[i]);   // an infinity has no remainder
+    }
+    if (v != v) p[0] = 0x7FC00000u;
+}
+
+__device__ __forceinline__ void eight(const uint4 (&r)[1], float (&f)[8])
+{
+    const uint32_t w[4] = {r[0].x, r[0].y, r[0].z, r[0].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(w[e] << 16); f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void eight(const uint4 (&r)[2], float (&f)[8])
+{
+    const uint32_t w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[1].x, r[1].y, r[1].z, r[1].w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(w[e]);
+}
+
+// The rows stay in registers and the matrix streams past them.  A workgroup has a wavefront per slice of 128 indices (up to 8, each with SL
+// slices): it holds the fragments of its slices for 16 CT batch rows, made from z once, and per tile of 16 vocabulary rows loads 16 bytes per
+// lane and slice, turns them into four fragments and feeds 4 CT PARTS matrix instructions.  The slices' partial tiles meet in LDS, RT tiles at
+// a time, and are summed in slice order; the row's 1 / rms is applied to the sum.  No element of z is read or split twice by a workgroup, and
+// nothing but partial tiles goes through LDS.
+// Bound: for few rows the matrix (17 bytes per 32 weights); from some 64 rows on the matrix instructions.
+// grid (<= groups of RT tiles, batch tiles of 16 CT), block 64 NW.
+template <typename T, int PARTS, int CT, int SL, int RT>
+__global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ exps,
+                                                       const T *__restrict__ gain, const T *__restrict__ z, long long z_stride,
+                                                       float *__restrict__ logits, int B, int d, int vocab, float eps, int norm_free)
+{
+    extern __shared__ __align__(16) unsigned char mx_smem[];
+    const int NW = blockDim.x >> 6;
+    float *ssq = reinterpret_cast<float *>(mx_smem);                                 // [8][16 CT] sums of squares, slice by slice
+    f32x4_t *part = reinterpret_cast<f32x4_t *>(mx_smem + 9 * 16 * CT * 4);          // [2][RT][NW][16 CT][4]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, g = lane >> 4;
+    const int b0 = blockIdx.y * 16 * CT, blocks = d / kMx4Block;
+    const int groups = (vocab + 16 * RT - 1) / (16 * RT);
+    int blk[SL];
+#pragma unroll
+    for (int s = 0; s < SL; ++s) blk[s] = 4 * (wave + s * NW) + g;   // this lane's block of a row in each slice
+
+    uint4 wc[RT][SL];
+    int we[RT][SL];
+    auto request = [&](int grp) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const size_t row = (size_t)min((grp * RT + t) * 16 + col, vocab - 1);
+#pragma unroll
+            for (int s = 0; s < SL; ++s) {
+                const int at = min(blk[s], blocks - 1);
+                wc[t][s] = *reinterpret_cast<const uint4 *>(codes + row * (d / 2) + (size_t)at * 16);
+                we[t][s] = exps[row * blocks + at];
+            }
+        }
+    };
+    // loads come back in order: the first rows, then the matrix, which is on its way while the rows are split
+    constexpr int kRaw = sizeof(T) / 2;   // 16-byte pieces of eight elements
+    uint4 zraw[SL][4][kRaw], graw[SL][4][kRaw];
+    const bool has_gain = PARTS == 2 || (PARTS == 3 && gain);
+    auto request_rows = [&](int c) {
+        const T *zr = z + min(b0 + 16 * c + col, B - 1) * z_stride;   // columns beyond the batch repeat its last row (their results are dropped)
+#pragma unroll
+        for (int s = 0; s < SL; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < kRaw; ++r) {
+                    const int k = min(blk[s], blocks - 1) * kMx4Block + 8 * j + r * (16 / (int)sizeof(T));
+                    zraw[s][j][r] = *reinterpret_cast<const uint4 *>(zr + k);
+                    if (c == 0 && has_gain) graw[s][j][r] = *reinterpret_cast<const uint4 *>(gain + k);
+                }
+    };
+    request_rows(0);
+    __builtin_amdgcn_sched_barrier(0);
+    int grp = blockIdx.x;
+    request(grp);
+    __builtin_amdgcn_sched_barrier(0);
+
+    Frag x[CT][SL][4][PARTS];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        if (c > 0) request_rows(c);
+        float ss = 0.f;
+#pragma unroll
+        for (int s = 0; s < SL; ++s) {
+            const bool in = blk[s] < blocks;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v[8], gn[8];
+                eight(zraw[s][j], v);
+                if (has_gain) eight(graw[s][j], gn);
+                uint32_t p[8][PARTS];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = in ? v[e] : 0.f;   // past the row's end
+                    ss = fmaf(v[e], v[e], ss);
+                    if (has_gain) v[e] *= gn[e];
+                    split_parts<PARTS>(v[e], p[e]);
+                }
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) {
+                    uint4 &u = x[c][s][j][i].u;
+                    u = make_uint4((p[0][i] >> 16) | p[1][i], (p[2][i] >> 16) | p[3][i], (p[4][i] >> 16) | p[5][i], (p[6][i] >> 16) | p[7][i]);
+                    asm("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));   // packed here: two values a register from now on
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);   // one block's loads at a time: the fragments take the registers
+        }
+        ss += xor16(ss);
+        ss += xor32(ss);
+        if (g == 0) ssq[wave * 16 * CT + 16 * c + col] = ss;
+    }
+    __syncthreads();
+    float *rinv = ssq + 8 * 16 * CT;   // [16 CT]
+    if (threadIdx.x < 16 * CT) {
+        float ss = 0.f;
+        for (int w = 0; w < NW; ++w) ss += ssq[w * 16 * CT + threadIdx.x];
+        rinv[threadIdx.x] = norm_free ? 1.f : rsqrtf(ss / (float)d + eps);   // read behind the loop's barrier
+    }
+    // the outputs of this thread: four vocabulary rows of one column, quad by quad and tile by tile
+    constexpr int kQuads = 4 * RT, kOut = 16 * CT * kQuads;
+    for (int buf = 0; grp < groups; buf ^= 1) {
+        f32x4_t *dst = part + (size_t)buf * RT * NW * 16 * CT * 4;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            f32x4_t acc[CT];
+#pragma unroll
+            for (int c = 0; c < CT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < SL; ++s) {
+                const float scale = __uint_as_float((uint32_t)we[t][s] << 23);
+                const bool in = blk[s] < blocks, odd = in && (we[t][s] == 0 || we[t][s] == 255);   // odd: no scale, the block reads as NaN
+                const uint32_t cw[4] = {wc[t][s].x, wc[t][s].y, wc[t][s].z, wc[t][s].w};
+                Frag a[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    a[j] = weight_fragment(in ? cw[j] : 0u, in ? scale : 1.f);
+                    if (odd) a[j].u = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
+                }
+#pragma unroll
+                for (int i = PARTS - 1; i >= 0; --i)   // the smallest part first
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) acc[c] = mfma16(a[j], x[c][s][j][i], acc[c]);
+            }
+#pragma unroll
+            for (int c = 0; c < CT; ++c)   // quads of a column turned by its number, so that 16 lanes of one quad meet all banks
+                dst[((size_t)(t * NW + wave) * 16 * CT + 16 * c + col) * 4 + ((g + (col >> 2)) & 3)] = acc[c];
+            __builtin_amdgcn_sched_barrier(0);   // tile by tile, for the same reason
+        }
+        const int now = grp;
+        grp += gridDim.x;
+        if (grp < groups) request(grp);
+        __syncthreads();   // one barrier per group: the next group's tiles go to the other half
+        for (int o = threadIdx.x; o < kOut; o += blockDim.x) {
+            const int quad = o & 3, t = (o >> 2) % RT, cc = o / kQuads, c16 = cc & 15;
+            if (b0 + cc >= B) continue;
+            f32x4_t sum = dst[((size_t)(t * NW) * 16 * CT + cc) * 4 + ((quad + (c16 >> 2)) & 3)];
+            for (int w = 1; w < NW; ++w) sum += dst[((size_t)(t * NW + w) * 16 * CT + cc) * 4 + ((quad + (c16 >> 2)) & 3)];
+            const int v0 = (now * RT + t) * 16 + 4 * quad;
+            float *out = logits + (size_t)(b0 + cc) * vocab + v0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (v0 + r < vocab) out[r] = sum[r] * rinv[cc];
+        }
+    }
+}
+
+template <typename T, int PARTS, int CT, int SL, int RT>
+static hipError_t mx4_rows_go(const uint8_t *codes, const uint8_t *exps, const T *g, const T *z, long long z_stride, float *logits, int B, int d,
+                              int vocab, float eps, int norm_free, hipStream_t st)
+{
+    const int slices = (d + 127) / 128, NW = (slices + SL - 1) / SL;
+    const size_t lds = 9 * 16 * CT * 4 + (size_t)2 * RT * NW * 16 * CT * 16 * 4;
+    const hipError_t e = hipFuncSetAttribute((const void *)mx4_rows_kernel<T, PARTS, CT, SL, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e != hipSuccess) return e;
+    const int groups = (vocab + 16 * RT - 1) / (16 * RT), chunks = (B + 16 * CT - 1) / (16 * CT);
+    const int most = CT >= 4 ? 256 : 512;
+    hipLaunchKernelGGL((mx4_rows_kernel<T, PARTS, CT, SL, RT>), dim3(groups < most ? groups : most, chunks), dim3(64 * NW), lds, st, codes, exps, g, z,
+                       z_stride, logits, B, d, vocab, eps, norm_free);
+    return hipGetLastError();
+}
+
+// ---- rows too wide for registers: staged in LDS as three parts, a tile of rows at a time.
+// grid (<= row tiles / 4, batch tiles of bt), block 256, LDS 3 bt ld bf16.
+constexpr size_t kMxMaxLds = 152 * 1024;
+
+__host__ __device__ static inline int mx_ld(int d) { return (d + 127) / 128 * 128 + 8; }   // a row's elements in LDS
+static_assert(3 * ((kMx4MaxWidth + 127) / 128 * 128 + 8) * 2 <= kMxMaxLds, "the widest row");
+
 template <typename T>
-__global__ __launch_bounds__(256) void mx4_head_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ exps,
+__global__ __launch_bounds__(256) void mx4_wide_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ exps,
                                                        const T *__restrict__ gain, const T *__restrict__ z, long long z_stride,
                                                        float *__restrict__ logits, int B, int d, int vocab, float eps, int norm_free, int bt)
 {
@@ -106,14 +308,10 @@ __global__ __launch_bounds__(256) void mx4_head_kernel(const uint8_t *__restrict
         for (int k = lane; k < ld; k += 64) {
             float v = 0.f;
             if (k < d) v = to_f32(zr[k]) * (rinv * ((gain && !norm_free) ? to_f32(gain[k]) : 1.f));
-            // by truncation, as a value beyond the largest bf16 has a finite head then; every difference is exact
-            const uint32_t p0 = __float_as_uint(v) & 0xFFFF0000u;
-            const float r1 = (p0 & 0x7F800000u) == 0x7F800000u ? 0.f : v - __uint_as_float(p0);   // an infinity has no remainder
-            const uint32_t p1 = __float_as_uint(r1) & 0xFFFF0000u;
-            const uint32_t p2 = __float_as_uint(r1 - __uint_as_float(p1));
-            zs[(size_t)b * ld + k] = v == v ? (bf16_t)(p0 >> 16) : (bf16_t)0x7FC0;
-            zs[(size_t)(bt + b) * ld + k] = (bf16_t)(p1 >> 16);
-            zs[(size_t)(2 * bt + b) * ld + k] = (bf16_t)(p2 >> 16);
+            uint32_t p[3];
+            split_parts<3>(v, p);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) zs[(size_t)(i * bt + b) * ld + k] = (bf16_t)(p[i] >> 16);
         }
     }
     __syncthreads();
@@ -135,9 +333,7 @@ __global__ __launch_bounds__(256) void mx4_head_kernel(const uint8_t *__restrict
             const uint32_t cw[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                Frag a, x;
-                a.u = make_uint4(two_weights<0>(cw[j], scale), two_weights<1>(cw[j], scale), two_weights<2>(cw[j], scale),
-                                 two_weights<3>(cw[j], scale));
+                Frag a = weight_fragment(cw[j], scale), x;
                 if (odd) a.u = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
                 const int k = 128 * st + 8 * j;
                 x.u = *reinterpret_cast<const uint4 *>(zl + k); low = mfma16(a, x, low);
@@ -164,15 +360,35 @@ template <typename T>
 hipError_t mx4_head_launch(const uint8_t *codes, const uint8_t *exps, const void *g, const void *z, long long z_stride, float *logits, int B,
                            int d, int vocab, float eps, int norm_free, hipStream_t st)
 {
+    const T *gt = norm_free ? nullptr : (const T *)g, *zt = (const T *)z;
+#define RT_MX4_GO(PARTS, CT, SL, RT_) return mx4_rows_go<T, PARTS, CT, SL, RT_>(codes, exps, gt, zt, z_stride, logits, B, d, vocab, eps, norm_free, st)
+    // the rows' 16-byte loads: anything else goes the way of the wide rows
+    const bool wide = d > 4096 || (z_stride * (long long)sizeof(T)) % 16 != 0 || ((uintptr_t)z & 15) != 0 || ((uintptr_t)g & 15) != 0;
+    if (wide) {
+    } else if constexpr (sizeof(T) == 2) {
+        if (gt) {
+            if (d <= 1024) { if (B <= 16) RT_MX4_GO(2, 1, 1, 4); if (B <= 32) RT_MX4_GO(2, 2, 1, 2); RT_MX4_GO(2, 4, 1, 2); }
+            if (d <= 2048) { if (B <= 16) RT_MX4_GO(2, 1, 2, 2); RT_MX4_GO(2, 2, 2, 2); }
+            RT_MX4_GO(2, 1, 4, 1);
+        } else {
+            if (d <= 1024) { if (B <= 16) RT_MX4_GO(1, 1, 1, 4); if (B <= 32) RT_MX4_GO(1, 2, 1, 2); RT_MX4_GO(1, 4, 1, 2); }
+            if (d <= 2048) { if (B <= 16) RT_MX4_GO(1, 1, 2, 2); RT_MX4_GO(1, 2, 2, 2); }
+            RT_MX4_GO(1, 1, 4, 1);
+        }
+    } else {
+        if (d <= 1024) { if (B <= 16) RT_MX4_GO(3, 1, 1, 4); RT_MX4_GO(3, 2, 1, 2); }
+        if (d <= 2048) RT_MX4_GO(3, 1, 2, 2);
+    }
+#undef RT_MX4_GO
     int bt = (int)(kMxMaxLds / ((size_t)3 * mx_ld(d) * 2));
     bt = bt > 16 ? 16 : bt;
     bt = bt > B ? B : bt;
     const size_t lds = (size_t)3 * bt * mx_ld(d) * 2;
-    hipError_t e = hipFuncSetAttribute((const void *)mx4_head_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMxMaxLds);
+    hipError_t e = hipFuncSetAttribute((const void *)mx4_wide_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kMxMaxLds);
     if (e != hipSuccess) return e;
     const int tiles = (vocab + 15) / 16, want = (tiles + 3) / 4;
     const int fit = (int)((size_t)160 * 1024 / lds), resident = 256 * (fit > 8 ? 8 : fit);
-    hipLaunchKernelGGL(mx4_head_kernel<T>, dim3(want < resident ? want : resident, (B + bt - 1) / bt), dim3(256), lds, st, codes, exps,
+    hipLaunchKernelGGL(mx4_wide_kernel<T>, dim3(want < resident ? want : resident, (B + bt - 1) / bt), dim3(256), lds, st, codes, exps,
                        (const T *)g, (const T *)z, z_stride, logits, B, d, vocab, eps, norm_free, bt);
     return hipGetLastError();
 }

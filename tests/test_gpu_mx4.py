@@ -10,8 +10,8 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 
-def _run(dtype, codes, exps, g, z, norm_free=False):
-    """z [B, 3, d]: rows at a stride, the middle ones are read."""
+def _run(dtype, codes, exps, g, z, norm_free=False, shift=0):
+    """z [B, 3, d]: rows at a stride, the middle ones are read; shift: they start that many elements on, the stride is odd."""
     from paper_2604_21215_amd import binding, torch_io as tio
     if not torch.cuda.is_available():
         pytest.fail("no GPU visible")
@@ -20,7 +20,8 @@ def _run(dtype, codes, exps, g, z, norm_free=False):
     ctx = binding.RTContext(d, d // 64, 64, B, 1, dtype, rms_eps=1e-6, flags=binding.RT_FLAG_NORM_FREE if norm_free else 0,
                             stream=torch.cuda.current_stream().cuda_stream)
     try:
-        zd = tio.to_device(z, dtype)
+        zd = tio.to_device(np.pad(z.reshape(B, 3 * d), ((0, 0), (shift, shift and 1 - shift % 2))), dtype)[:, shift:shift + 3 * d]
+        zd = zd.unflatten(1, (3, d))
         out = torch.full((B + 1, vocab), 7.0, dtype=torch.float32, device="cuda:0")
         ctx.rt_lm_head_mx4(torch.from_numpy(codes).to("cuda:0"), torch.from_numpy(exps).to("cuda:0"),
                            None if g is None else tio.to_device(g, dtype), zd[:, 1], zd.stride(0), B, out[:B])
@@ -36,7 +37,9 @@ def _run(dtype, codes, exps, g, z, norm_free=False):
     ("bf16", 64, 1, 1, False, True), ("bf16", 128, 15, 16, False, True), ("bf16", 192, 333, 17, False, False), ("bf16", 1024, 2064, 8, False, True),
     ("bf16", 1024, 50, 1, False, True), ("bf16", 512, 4097, 33, True, True), ("f32", 128, 1000, 3, False, True), ("f32", 320, 130, 40, False, True),
     ("f32", 64, 17, 2, True, False), ("bf16", 4096, 70, 5, False, True), ("bf16", 25856, 20, 2, False, True), ("bf16", 1024, 33000, 2, False, True),
-    ("bf16", 768, 515, 100, False, True)])
+    ("bf16", 768, 515, 100, False, True), ("bf16", 2048, 100, 16, False, True), ("bf16", 1536, 300, 40, False, False), ("bf16", 1088, 90, 3, False, True),
+    ("bf16", 3136, 100, 20, False, False), ("bf16", 576, 3000, 64, False, False), ("f32", 1024, 200, 20, False, True), ("f32", 1600, 70, 2, False, True),
+    ("f32", 2112, 70, 18, False, False), ("bf16", 4160, 33, 1, True, True), ("bf16", 128, 20000, 65, False, True)])
 def test_lm_head_mx4(dtype, d, vocab, B, norm_free, gain):
     from paper_2604_21215_amd import binding
     rng = np.random.default_rng(d + vocab + B)
@@ -59,6 +62,20 @@ def test_lm_head_mx4(dtype, d, vocab, B, norm_free, gain):
     # norm-wise: the rows' three roundings, the two of 1 / rms (common to a row) and the last sums are 2^-22 at most; each of four running
     # sums rounds d / 128 times at up to half of 2^-24 of itself, at random.  Rows rounded to bf16 would be off by 2^-9 / sqrt(3).
     assert np.linalg.norm(got - ref) <= (2.0 ** -22 + 2.0 ** -25 * np.sqrt(d / 128)) * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("dtype,d,B", [("bf16", 1024, 3), ("f32", 128, 17), ("bf16", 64, 1)])
+def test_rows_off_16_bytes(dtype, d, B):
+    from paper_2604_21215_amd import binding
+    rng = np.random.default_rng(B)
+    codes, exps = binding.rt_mx4_pack((rng.standard_normal((77, d)) * 0.05).astype(np.float32))
+    g, z = rng.uniform(0.5, 1.5, d).astype(np.float32), rng.standard_normal((B, 3, d)).astype(np.float32)
+    if dtype == "bf16":
+        g, z = gen.round_to_bf16(g), gen.round_to_bf16(z)
+    a, b = _run(dtype, codes, exps, g, z), _run(dtype, codes, exps, g, z, shift=3)
+    n = z[:, 1].astype(np.float64) / np.sqrt((z[:, 1].astype(np.float64) ** 2).mean(-1, keepdims=True) + 1e-6) * g.astype(np.float64)
+    bound = (8 * np.sqrt(d) + d / 64) * 2.0 ** -24 * (np.abs(n) @ np.abs(mx4_values(codes, exps)).T)
+    assert np.all(np.abs(a - b) <= 2 * bound) and np.all(np.abs(b - n @ mx4_values(codes, exps).T) <= bound)
 
 
 def test_every_code_and_scale():
