@@ -68,7 +68,7 @@ bool mx4_pack_host(const void *W, bool bf16, long long rows, int cols, uint8_t *
 }
 
 // ---------------------------------------------------------------- logits (device)
-// logits[b][v] = sum_k W[v][k] n_b[k], n_b = g z_b / rms(z_b): D[16 vocabulary rows][16 batch columns] += W[16][32] n^T[32][16].
+// logits[b][v] = sum_k W[v][k] n_b[k], n_b = g z_b / rms(z_b): products of 16 batch rows, 16 vocabulary rows and 32 indices.
 // The weights are exact in bf16 (two bits and a power of two), and one instruction turns two codes into two bf16 with their scale.  A lane
 // holds one whole block of a row: its 16 bytes of codes are four fragments, and the contraction index is dealt so that slot 8 g + e of
 // instruction j is k = 128 slice + 32 g + 8 j + e for lane group g.
@@ -89,16 +89,18 @@ __device__ __forceinline__ Frag weight_fragment(uint32_t codes, float scale)
     return f;
 }
 
-// v as the sum of PARTS bf16 values, by truncation: a value beyond the largest bf16 has a finite head then, and every difference is exact
+// v as the sum of PARTS bf16 values, by truncation: a value beyond the largest bf16 has a finite head then, and every difference is exact.
+// Two parts are taken of rows that are normalised: what is not finite reaches the logits through the row's 1 / rms.
 template <int PARTS> __device__ __forceinline__ void split_parts(float v, uint32_t (&p)[PARTS])
 {
     float r = v;
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) {
         p[i] = __float_as_uint(r) & 0xFFFF0000u;
-        r = (p[i] & 0x7F800000u) == 0x7F800000u ? 0.f : r - __uint_as_float(p[i]);   // an infinity has no remainder
+        r -= __uint_as_float(p[i]);
+        if (PARTS > 2) r = (p[i] & 0x7F800000u) == 0x7F800000u ? 0.f : r;   // an infinity has no remainder
     }
-    if (v != v) p[0] = 0x7FC00000u;
+    if (PARTS > 2 && v != v) p[0] = 0x7FC00000u;
 }
 
 __device__ __forceinline__ void eight(const uint4 (&r)[1], float (&f)[8])
@@ -140,6 +142,8 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
 
     uint4 wc[RT][SL];
     int we[RT][SL];
+    uint4 nc[RT][SL];
+    int ne[RT][SL];
     auto request = [&](int grp) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
@@ -147,8 +151,8 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
 #pragma unroll
             for (int s = 0; s < SL; ++s) {
                 const int at = min(blk[s], blocks - 1);
-                wc[t][s] = *reinterpret_cast<const uint4 *>(codes + row * (d / 2) + (size_t)at * 16);
-                we[t][s] = exps[row * blocks + at];
+                nc[t][s] = *reinterpret_cast<const uint4 *>(codes + row * (d / 2) + (size_t)at * 16);
+                ne[t][s] = exps[row * blocks + at];
             }
         }
     };
@@ -185,17 +189,25 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
             const bool in = blk[s] < blocks;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
+                if (!in) {   // past the row's end
+#pragma unroll
+                    for (int r = 0; r < kRaw; ++r) zraw[s][j][r] = make_uint4(0u, 0u, 0u, 0u);
+                }
                 float v[8], gn[8];
                 eight(zraw[s][j], v);
                 if (has_gain) eight(graw[s][j], gn);
-                uint32_t p[8][PARTS];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    v[e] = in ? v[e] : 0.f;   // past the row's end
                     ss = fmaf(v[e], v[e], ss);
                     if (has_gain) v[e] *= gn[e];
-                    split_parts<PARTS>(v[e], p[e]);
                 }
+                if (PARTS == 1) {   // bf16 as it is
+                    x[c][s][j][0].u = zraw[s][j][0];
+                    continue;
+                }
+                uint32_t p[8][PARTS];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) split_parts<PARTS>(v[e], p[e]);
 #pragma unroll
                 for (int i = 0; i < PARTS; ++i) {
                     uint4 &u = x[c][s][j][i].u;
@@ -216,10 +228,35 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
         for (int w = 0; w < NW; ++w) ss += ssq[w * 16 * CT + threadIdx.x];
         rinv[threadIdx.x] = norm_free ? 1.f : rsqrtf(ss / (float)d + eps);   // read behind the loop's barrier
     }
-    // the outputs of this thread: four vocabulary rows of one column, quad by quad and tile by tile
-    constexpr int kQuads = 4 * RT, kOut = 16 * CT * kQuads;
+    // Sums of a group's partial tiles: a thread takes one vocabulary row of four batch rows, neighbours neighbouring vocabulary rows.
+    constexpr int kOut = 16 * RT * 4 * CT;
+    auto finish = [&](const f32x4_t *src, int group) {
+        for (int o = threadIdx.x; o < kOut; o += blockDim.x) {
+            const int v = group * RT * 16 + o % (16 * RT), t = (o >> 4) % RT, q = o / (16 * RT);
+            if (b0 + 4 * q >= B || v >= vocab) continue;
+            const f32x4_t *p = src + (t * NW * 4 * CT + q) * 16 + (o & 15);
+            f32x4_t sum = p[0];
+            for (int w = 1; w < NW; ++w) sum += p[w * 4 * CT * 16];
+            float *out = logits + (size_t)(b0 + 4 * q) * vocab + v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (b0 + 4 * q + r < B) out[(size_t)r * vocab] = sum[r] * rinv[4 * q + r];
+        }
+    };
+    // Half of the wavefronts finish the group before while the other half, on the same SIMDs, keep the matrix units busy, and the other way
+    // round: one barrier per group, partial tiles in two halves.
+    const bool early = wave < 4;
+    int last = -1;
     for (int buf = 0; grp < groups; buf ^= 1) {
-        f32x4_t *dst = part + (size_t)buf * RT * NW * 16 * CT * 4;
+        f32x4_t *dst = part + buf * RT * NW * 16 * CT * 4, *prev = part + (buf ^ 1) * RT * NW * 16 * CT * 4;
+        const int now = grp;
+        grp += gridDim.x;
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int s = 0; s < SL; ++s) { wc[t][s] = nc[t][s]; we[t][s] = ne[t][s]; }
+        if (grp < groups) request(grp);   // a whole group ahead
+        if (early && last >= 0) finish(prev, last);
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             f32x4_t acc[CT];
@@ -241,28 +278,16 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int c = 0; c < CT; ++c) acc[c] = mfma16(a[j], x[c][s][j][i], acc[c]);
+                        for (int c = 0; c < CT; ++c) acc[c] = mfma16(x[c][s][j][i], a[j], acc[c]);
             }
 #pragma unroll
-            for (int c = 0; c < CT; ++c)   // quads of a column turned by its number, so that 16 lanes of one quad meet all banks
-                dst[((size_t)(t * NW + wave) * 16 * CT + 16 * c + col) * 4 + ((g + (col >> 2)) & 3)] = acc[c];
+            for (int c = 0; c < CT; ++c) dst[((t * NW + wave) * 4 * CT + 4 * c + g) * 16 + col] = acc[c];   // batch rows 4 g .., vocabulary row col
             __builtin_amdgcn_sched_barrier(0);   // tile by tile, for the same reason
         }
-        const int now = grp;
-        grp += gridDim.x;
-        if (grp < groups) request(grp);
-        __syncthreads();   // one barrier per group: the next group's tiles go to the other half
-        for (int o = threadIdx.x; o < kOut; o += blockDim.x) {
-            const int quad = o & 3, t = (o >> 2) % RT, cc = o / kQuads, c16 = cc & 15;
-            if (b0 + cc >= B) continue;
-            f32x4_t sum = dst[((size_t)(t * NW) * 16 * CT + cc) * 4 + ((quad + (c16 >> 2)) & 3)];
-            for (int w = 1; w < NW; ++w) sum += dst[((size_t)(t * NW + w) * 16 * CT + cc) * 4 + ((quad + (c16 >> 2)) & 3)];
-            const int v0 = (now * RT + t) * 16 + 4 * quad;
-            float *out = logits + (size_t)(b0 + cc) * vocab + v0;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (v0 + r < vocab) out[r] = sum[r] * rinv[cc];
-        }
+        if (!early && last >= 0) finish(prev, last);
+        last = now;
+        __syncthreads();
+        if (grp >= groups) finish(dst, now);
     }
 }
 
