@@ -351,40 +351,58 @@ class RTContext:
                                 _ptr(logits))
         _check(self._L, self._ctx, rc)
 
+    # The calls of a serving loop pass addresses as plain integers: a ctypes object per pointer costs as much as the call itself.
+
     # -- rt_cache_write(ctx, cache, S, first[S] int32, count[S] int32 | None, N, k[S,N,H,64], v, seq_stride, pos_stride)
     def rt_cache_write(self, cache: rt_paged_cache, first, count, k, v):
-        rc = self._L.rt_cache_write(self._ctx, C.byref(cache), k.shape[0], _ptr(first), _ptr(count), k.shape[1], _ptr(k), _ptr(v),
-                                    *_pair_strides(k, v))
-        _check(self._L, self._ctx, rc)
+        S, N = k.shape[:2]
+        ss, ps = _pair_strides(k, v)
+        rc = self._L.rt_cache_write(self._ctx, cache, S, first.data_ptr(), None if count is None else count.data_ptr(), N, k.data_ptr(),
+                                    v.data_ptr(), ss, ps)
+        if rc:
+            _check(self._L, self._ctx, rc)
 
     # -- rt_cache_read(ctx, cache, S, first[S] int32, count[S] int32 | None, N, k[S,N,H,64], v, seq_stride, pos_stride)
     def rt_cache_read(self, cache: rt_paged_cache, first, count, k, v):
-        rc = self._L.rt_cache_read(self._ctx, C.byref(cache), k.shape[0], _ptr(first), _ptr(count), k.shape[1], _ptr(k), _ptr(v),
-                                   *_pair_strides(k, v))
-        _check(self._L, self._ctx, rc)
+        S, N = k.shape[:2]
+        ss, ps = _pair_strides(k, v)
+        rc = self._L.rt_cache_read(self._ctx, cache, S, first.data_ptr(), None if count is None else count.data_ptr(), N, k.data_ptr(),
+                                   v.data_ptr(), ss, ps)
+        if rc:
+            _check(self._L, self._ctx, rc)
 
     # -- rt_paged_attention(ctx, cache, S, lens[S] int32, max_len, q[S,H,64], q_stride, k_t | None, v_t | None, kv_stride, out, out_stride, lse[S,H] f32 | None)
     def rt_paged_attention(self, cache: rt_paged_cache, lens, max_len, q, k_t, v_t, out, lse=None):
         """q, k_t, v_t, out [S, H, 64] (or [S, d]): rows at their first stride, contiguous inside."""
         S, d = q.shape[0], self.cfg.d_model
-        stride = lambda t: t.stride(0) if S > 1 else d  # noqa: E731
-        if k_t is not None and v_t is not None and stride(k_t) != stride(v_t):
-            raise RTError("RT_ERR_INVALID_ARG", "k_t and v_t have one stride")
-        rc = self._L.rt_paged_attention(self._ctx, C.byref(cache), S, _ptr(lens), int(max_len), _ptr(q), stride(q), _ptr(k_t), _ptr(v_t),
-                                        stride(k_t) if k_t is not None else d, _ptr(out), stride(out), _ptr(lse))
-        _check(self._L, self._ctx, rc)
+        qs, os_, ks, kp, vp = d, d, d, None, None
+        if S > 1:   # a dimension of one row has no stride
+            qs, os_ = q.stride(0), out.stride(0)
+        if k_t is not None:
+            kp = k_t.data_ptr()
+            if S > 1:
+                ks = k_t.stride(0)
+        if v_t is not None:
+            vp = v_t.data_ptr()
+            if S > 1 and k_t is not None and v_t.stride(0) != ks:
+                raise RTError("RT_ERR_INVALID_ARG", "k_t and v_t have one stride")
+        rc = self._L.rt_paged_attention(self._ctx, cache, S, lens.data_ptr(), max_len, q.data_ptr(), qs, kp, vp, ks, out.data_ptr(), os_,
+                                        None if lse is None else lse.data_ptr())
+        if rc:
+            _check(self._L, self._ctx, rc)
 
     # -- rt_decode_step_paged(ctx, w, cache, x_t[S,d], S, pos[S] int32, max_pos, y_t[S,d])
     def rt_decode_step_paged(self, weights: rt_layer_weights, cache: rt_paged_cache, x_t, pos, max_pos, y_t):
-        rc = self._L.rt_decode_step_paged(self._ctx, C.byref(weights), C.byref(cache), _ptr(x_t), x_t.shape[0], _ptr(pos), int(max_pos),
-                                          _ptr(y_t))
-        _check(self._L, self._ctx, rc)
+        rc = self._L.rt_decode_step_paged(self._ctx, weights, cache, x_t.data_ptr(), x_t.shape[0], pos.data_ptr(), max_pos, y_t.data_ptr())
+        if rc:
+            _check(self._L, self._ctx, rc)
 
     # -- rt_lm_head_mx4(ctx, codes[vocab,d/2], exps[vocab,d/32], g_final[d] | None, vocab, z rows, z_stride, B, logits[B,vocab] f32)
     def rt_lm_head_mx4(self, codes, exps, g_final, z, z_stride, B, logits):
-        rc = self._L.rt_lm_head_mx4(self._ctx, _ptr(codes), _ptr(exps), _ptr(g_final), codes.shape[0], _ptr(z), int(z_stride), int(B),
-                                    _ptr(logits))
-        _check(self._L, self._ctx, rc)
+        rc = self._L.rt_lm_head_mx4(self._ctx, codes.data_ptr(), exps.data_ptr(), None if g_final is None else g_final.data_ptr(),
+                                    codes.shape[0], z.data_ptr(), z_stride, B, logits.data_ptr())
+        if rc:
+            _check(self._L, self._ctx, rc)
 
     # -- rt_cross_block_event(ctx, K, V, B, t1, P, nq)
     def rt_cross_block_event(self, K, V, t1, P, nq):

@@ -158,7 +158,7 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
     };
     // loads come back in order: the first rows, then the matrix, which is on its way while the rows are split
     constexpr int kRaw = sizeof(T) / 2;   // 16-byte pieces of eight elements
-    uint4 zraw[SL][4][kRaw], graw[SL][4][kRaw];
+    uint4 znext[SL][4][kRaw], graw[SL][4][kRaw];
     const bool has_gain = PARTS == 2 || (PARTS == 3 && gain);
     auto request_rows = [&](int c) {
         const T *zr = z + min(b0 + 16 * c + col, B - 1) * z_stride;   // columns beyond the batch repeat its last row (their results are dropped)
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
 #pragma unroll
                 for (int r = 0; r < kRaw; ++r) {
                     const int k = min(blk[s], blocks - 1) * kMx4Block + 8 * j + r * (16 / (int)sizeof(T));
-                    zraw[s][j][r] = *reinterpret_cast<const uint4 *>(zr + k);
+                    znext[s][j][r] = *reinterpret_cast<const uint4 *>(zr + k);
                     if (c == 0 && has_gain) graw[s][j][r] = *reinterpret_cast<const uint4 *>(gain + k);
                 }
     };
@@ -182,7 +182,14 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
     Frag x[CT][SL][4][PARTS];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        if (c > 0) request_rows(c);
+        uint4 zraw[SL][4][kRaw];
+#pragma unroll
+        for (int s = 0; s < SL; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < kRaw; ++r) zraw[s][j][r] = znext[s][j][r];
+        if (c + 1 < CT) request_rows(c + 1);
         float ss = 0.f;
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
@@ -235,8 +242,13 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
             const int v = group * RT * 16 + o % (16 * RT), t = (o >> 4) % RT, q = o / (16 * RT);
             if (b0 + 4 * q >= B || v >= vocab) continue;
             const f32x4_t *p = src + (t * NW * 4 * CT + q) * 16 + (o & 15);
-            f32x4_t sum = p[0];
-            for (int w = 1; w < NW; ++w) sum += p[w * 4 * CT * 16];
+            f32x4_t s[8];
+#pragma unroll
+            for (int w = 0; w < 8; ++w) s[w] = p[min(w, NW - 1) * 4 * CT * 16];   // all on the way before the first is added
+            f32x4_t sum = s[0];
+#pragma unroll
+            for (int w = 1; w < 8; ++w)
+                if (w < NW) sum += s[w];
             float *out = logits + (size_t)(b0 + 4 * q) * vocab + v;
 #pragma unroll
             for (int r = 0; r < 4; ++r)

@@ -46,7 +46,6 @@ struct PagedAttention {
 
 template <typename T> hipError_t cache_write_launch(const PagedCache &C, const PairRows &R, int H, const void *k, const void *v, hipStream_t st);
 template <typename T> hipError_t cache_read_launch(const PagedCache &C, const PairRows &R, int H, void *k, void *v, hipStream_t st);
-SplitPlan paged_plan(int max_len, int S, int H);
 size_t paged_partials_bytes();
 void paged_partials(PagedAttention &A, void *slab);
 template <typename T> hipError_t paged_attention_launch(const PagedCache &C, const PagedAttention &A, hipStream_t st);

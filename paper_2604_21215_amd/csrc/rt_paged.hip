@@ -7,6 +7,8 @@
 #include "rt_paged.h"
 #include "rt_ll.h"
 
+#include <type_traits>
+
 namespace rt {
 
 // ---------------------------------------------------------------- rows of 64 values, 16 bytes of them per lane
@@ -256,37 +258,43 @@ __device__ __forceinline__ void finish_row(const PagedAttention &A, int s, int h
     }
 }
 
-// C: type of the cached values (T or int8_t).  Workgroup = (split, h, s), its four wavefronts share the split's rows in four runs.
-// A wavefront loads NL times 64 / LPR rows of keys and of values before it computes on them.
+// C: type of the cached values (T or int8_t).  Workgroup = (h, s, split), heads first: consecutive workgroups go to different XCDs, and all
+// heads of a sequence have the same work, while the late splits of a ragged batch are mostly empty (splits first, and eight of them: an
+// XCD gets one split of every sequence, 512 pairs of up to 8000 positions: 125 us instead of 98).  Its four wavefronts share the split's rows in four runs.
+// A wavefront loads 64 rows of keys and of values (fp32: 32), or 16 where no more are left, before it computes on them.
 template <typename T, typename C, bool STEP>
 __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P, const PagedAttention A)
 {
-    constexpr int LPR = kLanesPerRow<C>, PL = kPerLane<C>, RPL = 64 / LPR, NL = sizeof(C) == 1 ? 4 : 8, CH = NL * RPL;
+    constexpr int LPR = kLanesPerRow<C>, PL = kPerLane<C>, RPL = 64 / LPR, NL = sizeof(C) == 1 ? 4 : 8, CH = NL * RPL, SMALL = 16 / RPL;
     constexpr bool Q8 = sizeof(C) == 1;
     __shared__ float sm[4 * RPL], sl[4 * RPL];
     __shared__ float so[4 * RPL][kHeadDim];
     __shared__ int sbad[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int split = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
-    const int n = A.lens[s];
+    const int split = blockIdx.z, h = blockIdx.x, s = blockIdx.y;
     const int lo = split * A.plan.split_len;
     const bool one = A.plan.n_splits == 1;
+    // requested together: the length, the token's rows, the table's first 64 entries of this split (whether they are needed or not)
+    const int32_t *line = P.table + s * P.table_stride;
+    const int n = A.lens[s];
+    int base = lo >> P.lg, have = 64;   // lane i holds the entry of page base + i of the sequence, i < have
+    int entry = line[min((long long)base + lane, P.table_stride - 1)];
+    TokenRows<T, STEP> tok(A, s, h);
     if (n < 0 || n > A.max_len) {
         if (split == 0 && wave == 0 && (STEP || n > 0)) {   // an idle row of a step: zeros for the products; too long: NaN
-            TokenRows<T, STEP> t(A, s, h);
-            t.pair = false;
-            finish_row<T, STEP>(A, s, h, t, kLowest, 0.f, 0.f, n > 0);
+            tok.pair = false;
+            finish_row<T, STEP>(A, s, h, tok, kLowest, 0.f, 0.f, n > 0);
         }
         return;
     }
     if (lo >= n && !one) return;   // no rows here; the join counts the splits in the same way
     const int hi = min(n, lo + A.plan.split_len);
-    // this wavefront's run: a quarter of the rows in whole chunks
-    const int share = ((hi - lo + 4 * CH - 1) / (4 * CH)) * CH;
+    // this wavefront's run: a quarter of the rows, in whole chunks where there is more than one for each
+    const int unit = hi - lo > 4 * 16 ? CH : 16;
+    const int share = ((hi - lo + 4 * unit - 1) / (4 * unit)) * unit;
     const int wlo = lo + wave * share, whi = min(hi, wlo + share);
 
     const int c = lane % LPR, g = lane / LPR;
-    TokenRows<T, STEP> tok(A, s, h);
     float q[PL];
 #pragma unroll
     for (int e = 0; e < PL; ++e) q[e] = __shfl(tok.q, c * PL + e, 64);
@@ -295,26 +303,23 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P
     for (int e = 0; e < PL; ++e) o[e] = 0.f;
     const float slope = alibi_slope(A.alibi, h, A.H);
     bool bad = false;
-    const int last_page = (n - 1) >> P.lg;
-    const int32_t *line = P.table + s * P.table_stride;
-    int base = 0, entry = 0, have = 0;   // lane i holds the entry of page base + i of the sequence, i < have
-    for (int r0 = wlo; r0 < whi; r0 += CH) {
-        if (((r0 + CH - 1) >> P.lg) >= base + have) {
-            base = r0 >> P.lg;
-            have = 64;
-            const int p = min(base + lane, last_page);
-            entry = line[p];
-            const bool wrong = !page_ok(entry, P.pages);
-            if (wrong) entry = 0;
-            bad = bad || __any(wrong && ((base + lane) << P.lg) < whi);
-        }
-        uint4 kr[NL], vr[NL];
-        float ks[NL], vs[NL];
+    const int last_page = max(n - 1, 0) >> P.lg, page_mask = (1 << P.lg) - 1;
+    auto check_entries = [&] {   // entries that name no page are not followed; the ones that this run needs make the row NaN
+        const bool wrong = !page_ok(entry, P.pages);
+        if (wrong) entry = 0;
+        const int p = base + lane;
+        bad = bad || __any(wrong && p >= (wlo >> P.lg) && p <= last_page && ((long long)p << P.lg) < whi);
+    };
+    check_entries();
+    auto chunk = [&](int r0, auto loads) {
+        constexpr int N = decltype(loads)::value;
+        uint4 kr[N], vr[N];
+        float ks[N], vs[N];
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
+        for (int i = 0; i < N; ++i) {
             const int r = r0 + i * RPL;
             const int page = __builtin_amdgcn_readlane(entry, min(r >> P.lg, last_page) - base);
-            const size_t row = pool_row(page, A.H, h, P.lg, r & ((1 << P.lg) - 1)) + g;
+            const size_t row = pool_row(page, A.H, h, P.lg, r & page_mask) + g;
             kr[i] = *reinterpret_cast<const uint4 *>((const C *)P.K + row * kHeadDim + c * PL);
             vr[i] = *reinterpret_cast<const uint4 *>((const C *)P.V + row * kHeadDim + c * PL);
             if (Q8) {
@@ -322,9 +327,9 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P
                 vs[i] = __uint_as_float(exponent_step_bits(P.Vx[row]));
             }
         }
-        float z[NL], mx = m;
+        float z[N], mx = m;
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
+        for (int i = 0; i < N; ++i) {
             float f[PL], acc = 0.f;
             widen(kr[i], f, (const C *)nullptr);
 #pragma unroll
@@ -340,7 +345,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P
 #pragma unroll
         for (int e = 0; e < PL; ++e) o[e] *= f0;
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
+        for (int i = 0; i < N; ++i) {
             const float p = exp_diff(z[i], mx);
             l += p;
             float f[PL];
@@ -351,6 +356,15 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P
             for (int e = 0; e < PL; ++e) o[e] = fmaf(w, Q8 || in ? f[e] : 0.f, o[e]);
         }
         m = mx;
+    };
+    for (int r0 = wlo; r0 < whi; r0 += CH) {
+        if ((min(r0 + CH, whi) - 1) >> P.lg >= base + have) {
+            base = r0 >> P.lg;
+            entry = line[min(base + lane, last_page)];
+            check_entries();
+        }
+        if (whi - r0 > 16) chunk(r0, std::integral_constant<int, NL>{});
+        else chunk(r0, std::integral_constant<int, SMALL>{});
     }
     // the groups' states meet in LDS
     const int grp = wave * RPL + g;
@@ -368,6 +382,7 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P
     float L = lane < 4 * RPL ? sl[lane] * exp_diff(sm[lane], M) : 0.f;
     L = fast_sum(L);
     float O = 0.f;
+#pragma unroll 16
     for (int i = 0; i < 4 * RPL; ++i) O += so[i][lane];
     const bool any_bad = sbad[0] | sbad[1] | sbad[2] | sbad[3];
     if (one) {
@@ -380,39 +395,64 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P
     A.po[idx * kHeadDim + lane] = O;
 }
 
-// The splits of every (s, h) joined, one wavefront each: the largest maximum first, then the weighted sums in split order.
+// The splits of every (s, h) joined, one wavefront each: the largest maximum first, then the weighted sums in split order.  The stored
+// sums are requested before the maxima are known, 64 splits at a time, four per instruction (sixteen lanes each).
 // grid ceil(S H / 4), block 256.
 template <typename T, bool STEP> __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttention A)
 {
     const int lane = threadIdx.x & 63, sh = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (sh >= A.S * A.H) return;
-    const int s = sh / A.H, h = sh % A.H;
+    const int s = sh / A.H, h = sh % A.H, all = A.plan.n_splits;
+    const float *pm = A.pm + (size_t)sh * all, *pl = A.pl + (size_t)sh * all;
+    const float *po = A.po + (size_t)sh * all * kHeadDim + (lane & 15) * 4;
     const int n = A.lens[s];
+    TokenRows<T, STEP> tok(A, s, h);
+    float m = kLowest, l = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
     if (n < 0 || n > A.max_len) return;   // done by the splits' launch
     const int ns = (n + A.plan.split_len - 1) / A.plan.split_len;
-    const float *pm = A.pm + (size_t)sh * A.plan.n_splits, *pl = A.pl + (size_t)sh * A.plan.n_splits;
-    const float *po = A.po + (size_t)sh * A.plan.n_splits * kHeadDim + lane;
-    TokenRows<T, STEP> tok(A, s, h);
-    float m = kLowest, l = 0.f, o = 0.f;
-    for (int i = lane; i < ns; i += 64) m = fmaxf(m, pm[i]);
-    m = fast_max(m);
     for (int i0 = 0; i0 < ns; i0 += 64) {
-        const int i = i0 + lane, cnt = min(64, ns - i0);
-        const float w = i < ns ? exp_diff(pm[i], m) : 0.f;
-        const float lw = i < ns ? w * pl[i] : 0.f;
-        l += fast_sum(lw);
-        for (int j0 = 0; j0 < cnt; j0 += 8) {   // eight state rows in flight
-            float v[8];
+        const int i = min(i0 + lane, all - 1);
+        const float mi = pm[i], li = pl[i];
+        constexpr int kHalf = 8;
+        f32x4_t v[2][kHalf];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = po[(size_t)(i0 + min(j0 + e, cnt - 1)) * kHeadDim];
+        for (int k = 0; k < kHalf; ++k) v[0][k] = *reinterpret_cast<const f32x4_t *>(po + (size_t)min(i0 + 4 * k + (lane >> 4), all - 1) * kHeadDim);
+        if (ns - i0 > 32) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o = fmaf(j0 + e < cnt ? lane_bcast(w, min(j0 + e, 63)) : 0.f, v[e], o);
+            for (int k = 0; k < kHalf; ++k)
+                v[1][k] = *reinterpret_cast<const f32x4_t *>(po + (size_t)min(i0 + 32 + 4 * k + (lane >> 4), all - 1) * kHeadDim);
         }
+        const bool in = i0 + lane < ns;
+        const float mx = fmaxf(m, fast_max(in ? mi : kLowest)), f0 = exp_diff(m, mx);
+        const float w = in ? exp_diff(mi, mx) : 0.f;
+        l = fmaf(l, f0, fast_sum(in ? w * li : 0.f));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] *= f0;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            if (half && ns - i0 <= 32) break;
+#pragma unroll
+            for (int k = 0; k < kHalf; ++k) {
+                const int j = 32 * half + 4 * k + (lane >> 4);
+                const float wj = __shfl(w, j, 64);
+                const bool there = i0 + j < ns;   // what was not written may be anything
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = fmaf(wj, there ? v[half][k][r] : 0.f, o[r]);
+            }
+        }
+        m = mx;
     }
-    finish_row<T, STEP>(A, s, h, tok, m, l, o, false);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        o[r] += xor16(o[r]);
+        o[r] += xor32(o[r]);
+    }
+    const int src = lane >> 2;   // the lane that holds dimensions 4 (lane / 4) ..
+    const float o0 = __shfl(o[0], src, 64), o1 = __shfl(o[1], src, 64), o2 = __shfl(o[2], src, 64), o3 = __shfl(o[3], src, 64);
+    finish_row<T, STEP>(A, s, h, tok, m, l, lane & 2 ? (lane & 1 ? o3 : o2) : (lane & 1 ? o1 : o0), false);
 }
 
-SplitPlan paged_plan(int max_len, int S, int H) { return split_plan(max_len, S, H, 2048, 1024); }
 size_t paged_partials_bytes() { return (size_t)kMaxPartials * (kHeadDim + 2) * 4; }
 void paged_partials(PagedAttention &A, void *slab)
 {
@@ -423,7 +463,7 @@ void paged_partials(PagedAttention &A, void *slab)
 
 template <typename T, bool STEP> static hipError_t attention_launch(const PagedCache &C, const PagedAttention &A, hipStream_t st)
 {
-    const dim3 grid((unsigned)A.plan.n_splits, (unsigned)A.H, (unsigned)A.S);
+    const dim3 grid((unsigned)A.H, (unsigned)A.S, (unsigned)A.plan.n_splits);
     if (C.Kx) hipLaunchKernelGGL((paged_attention_kernel<T, int8_t, STEP>), grid, dim3(256), 0, st, C, A);
     else hipLaunchKernelGGL((paged_attention_kernel<T, T, STEP>), grid, dim3(256), 0, st, C, A);
     if (A.plan.n_splits > 1)

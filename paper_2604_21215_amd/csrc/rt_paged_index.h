@@ -38,21 +38,30 @@ RT_BOTH uint32_t exponent_step_bits(int byte) { return byte == 255 ? 0x7FC00000u
 RT_BOTH uint32_t exponent_inverse_bits(int byte) { return byte == 0 || byte == 255 ? 0u : (uint32_t)(254 - byte) << 23; }   // 2^-e, or 0
 
 // How the positions below max_len of S sequences and H heads are cut: workgroups of split_len positions each (the last one shorter).
+// A cut costs a second launch and a stored state per part.  Few pairs of a sequence and a head are cut until the chip has something to do
+// (kWantGroups workgroups, parts of kShort positions and more); and all of them into parts of about kLong, which bounds how long one
+// sequence of a ragged batch keeps its workgroup after the others are done.  MI355X, us per call, S H pairs of up to so many positions, by
+// the number of parts (bf16):
+//   16 pairs, 700: one 7.3, three 7.8;  1000: one 8.8, four 7.6;  64 pairs, 2000: one 14.5, four 9.3, eight 8.5;
+//   256 pairs, 1000: one 10.9, four 11.6;  2000: one 20.3, three 17.6, eight 18.4;  8000: one 72.7, four 45.7, six 41.5, sixteen 41.8;
+//   512 pairs, 2000: one 27.9, two 30.4, eight 28.4;  8000: one 114, two 97.5, eight 98.0, 32 99.2;  1600 pairs, 8000 (8 bits): one 188,
+//   eight 160, 32 181;  32 pairs, 100001: one 1021, eight 154, 24 113, 98 122.
 struct SplitPlan {
     int split_len, n_splits;
 };
 constexpr int kMaxPartials = 65536;    // stored partial states of a call: S * H * n_splits if n_splits > 1
 constexpr int kSplitUnit = 256;        // four wavefronts of 64 positions
-RT_BOTH SplitPlan split_plan(int max_len, int S, int H, int want_groups, int longest)
+constexpr int kWantGroups = 768, kShort = 256, kWhole = 640, kLong = 1024;
+RT_BOTH SplitPlan split_plan(int max_len, int S, int H)
 {
     const int64_t pairs = (int64_t)S * H;
-    int64_t want = (want_groups + pairs - 1) / pairs;                 // splits that fill the chip
-    const int64_t least = ((int64_t)max_len + longest - 1) / longest;  // splits that keep the longest sequence's share short
-    if (want < least) want = least;
-    const int64_t most = kMaxPartials / pairs;
-    if (want > most) want = most;
-    if (want < 1) want = 1;
-    int64_t len = ((int64_t)max_len + want - 1) / want;
+    int64_t n = kWantGroups / pairs;
+    const int64_t most = max_len <= kWhole ? 1 : (max_len + kShort - 1) / kShort;
+    if (n > most) n = most;
+    if (n < max_len / kLong) n = max_len / kLong;
+    if (n > kMaxPartials / pairs) n = kMaxPartials / pairs;
+    if (n < 1) n = 1;
+    int64_t len = ((int64_t)max_len + n - 1) / n;
     len = (len + kSplitUnit - 1) / kSplitUnit * kSplitUnit;
     if (len < kSplitUnit) len = kSplitUnit;
     SplitPlan p;

@@ -60,8 +60,8 @@ static int plans()
     for (int len : lens)
         for (int S : seqs)
             for (int H : heads)
-                for (int longest : {512, 1024, 4096}) {
-                    const SplitPlan p = split_plan(len, S, H, 2048, longest);
+                {
+                    const SplitPlan p = split_plan(len, S, H);
                     EXPECT(p.n_splits >= 1 && p.split_len >= kSplitUnit && p.split_len % kSplitUnit == 0);
                     EXPECT((int64_t)p.n_splits * p.split_len >= len);
                     EXPECT(p.n_splits == 1 || (int64_t)(p.n_splits - 1) * p.split_len < len);
