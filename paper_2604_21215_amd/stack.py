@@ -7,6 +7,7 @@ from __future__ import annotations
 import torch
 
 from . import binding
+from .paged import PagedCaches
 from .torch_io import DeviceLayer, to_device, torch_dtype
 
 
@@ -20,6 +21,7 @@ class DeviceStack:
         self.vocab, self.d = self.embedding.shape
         self.H = ctx.cfg.n_heads
         self.K = self.V = self.y = None
+        self.head4 = None
 
     def prefill(self, ids: torch.Tensor, N: int, kv_cap: int, keep_outputs: bool = True, wavefront: bool = False,
                 chunk: int = 0):
@@ -67,4 +69,35 @@ class DeviceStack:
             self.ctx.rt_decode_step(lay.struct, rows[l, :, 0], t, rows[l + 1, :, 0], self.K[l], self.V[l])
         logits = torch.empty((B, self.vocab), dtype=torch.float32, device=self.device)
         self.ctx.rt_lm_head(self.lm_head, self.g_final, rows[L], self.d, B, logits)
+        return logits, rows[1:, :, 0]
+
+    def pack_lm_head(self):
+        """The output projection in 4 bits beside the stored one (rt_mx4_pack on the host); decode_step_paged(head4=True) reads it."""
+        w = self.lm_head.view(torch.int16).cpu().numpy().view("uint16") if self.dtype == "bf16" else self.lm_head.cpu().numpy()
+        self.head4 = tuple(torch.from_numpy(a).to(self.device) for a in binding.rt_mx4_pack(w))
+
+    def into_pages(self, caches: PagedCaches, lens):
+        """The pairs that the last prefill left in self.K, self.V, rows 0 .. lens[b] - 1 of sequence b, into the pages of place b (which are
+        reserved here, with room for the next token).  lens[b] < 0: nothing of sequence b."""
+        caches.reserve([int(n) + 1 if n >= 0 else 0 for n in lens])
+        count = torch.tensor([max(int(n), 0) for n in lens], dtype=torch.int32, device=self.device)
+        first = torch.tensor([0 if n >= 0 else -1 for n in lens], dtype=torch.int32, device=self.device)
+        for l in range(len(self.layers)):
+            N = max(max(int(n) for n in lens), 1)
+            self.ctx.rt_cache_write(caches.layer[l], first, count, self.K[l][:N].transpose(0, 1), self.V[l][:N].transpose(0, 1))
+
+    def decode_step_paged(self, caches: PagedCaches, ids: torch.Tensor, pos: torch.Tensor, max_pos: int, head4: bool = False):
+        """One token of every sequence: ids [S] int32 on the device, sequence s at its own position pos[s] (int32 on the device, at most
+        max_pos; negative: an idle place, whose rows hold nothing).  The pages have been reserved for pos[s] + 1 positions.  Returns (logits
+        [S, vocab] fp32, per-layer outputs [L, S, d]); head4: the read-out with the 4-bit weights of pack_lm_head."""
+        S, L = ids.shape[0], len(self.layers)
+        rows = torch.zeros((L + 1, S, 1, self.d), dtype=torch_dtype(self.dtype), device=self.device)
+        self.ctx.rt_embed_rows(self.embedding, ids.view(S, 1), 0, rows[0])
+        for l, lay in enumerate(self.layers):
+            self.ctx.rt_decode_step_paged(lay.struct, caches.layer[l], rows[l, :, 0], pos, max_pos, rows[l + 1, :, 0])
+        logits = torch.empty((S, self.vocab), dtype=torch.float32, device=self.device)
+        if head4:
+            self.ctx.rt_lm_head_mx4(self.head4[0], self.head4[1], self.g_final, rows[L], self.d, S, logits)
+        else:
+            self.ctx.rt_lm_head(self.lm_head, self.g_final, rows[L], self.d, S, logits)
         return logits, rows[1:, :, 0]
