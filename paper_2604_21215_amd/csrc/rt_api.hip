@@ -1125,6 +1125,7 @@ extern "C" rt_status rt_stack_prefill(rt_ctx *c, const rt_layer_weights *layers,
         host[l].S = c->stack_S[l];
         host[l].x = l == 0 ? x : y[l - 1];
         host[l].y = y[l]; host[l].K = K[l]; host[l].V = V[l];
+        host[l].out = StepPages{};
         poison_partials(c, c->stack_S[l]);
     }
     LayerDims D = c->base;
@@ -1392,11 +1393,10 @@ static rt_status decode_paged(rt_ctx *c, LayerDims D, const rt_layer_weights *w,
     hipStream_t st = c->stream;
     Scratch S = c->S;
     S.Q = nullptr;   // the queries and the temporary pairs stay in fp32 rows
-    void *y_new = (char *)c->paged_slab + paged_rows_offset();
     const bool mm = sizeof(T) == 2 && step_mm_supported(D, c->use_mfma), wide = mm && step_uses_wide(D);
     if (wide) RT_TRY(step_qkv_wide(D, W, S, x_t, (size_t)D.d, st), "step_qkv_wide");
     else if (mm) RT_TRY(step_qkv_mm(D, W, S, x_t, (size_t)D.d, st), "step_qkv_mm");
-    else RT_TRY(Launch<T>::qkv_raw(D, W, S, x_t, (size_t)D.d, st), "qkv_raw");
+    else RT_TRY(paged_qkv_launch<T>(D, W, S, x_t, st), "paged_qkv");
     PagedAttention A = {};
     A.S = D.B; A.H = D.H; A.max_len = max_pos; A.lens = pos;
     A.scale = D.scale; A.alibi = D.alibi;
@@ -1406,15 +1406,14 @@ static rt_status decode_paged(rt_ctx *c, LayerDims D, const rt_layer_weights *w,
     paged_partials(A, c->paged_slab);
     A.plan = split_plan(max_pos, D.B, D.H);
     RT_TRY(paged_attention_launch<T>(C, A, st), "paged_attention");
-    if (mm) {
-        RT_TRY(step_base_case_mm(D, W, S, x_t, y_new, nullptr, nullptr, st), "step_base_case_mm");
-    } else {
-        RT_TRY(Launch<T>::gemv_wo(D, W, S, x_t, (size_t)D.d, st), "gemv_wo");
-        RT_TRY(Launch<T>::gemv_w1(D, W, S, st), "gemv_w1");
-        RT_TRY(Launch<T>::gemv_w2(D, W, S, y_new, (size_t)D.d, st), "gemv_w2");
-        RT_TRY(Launch<T>::gemv_kv(D, W, S, st), "gemv_kv");
+    if (mm) {   // the products' own epilogues end the step
+        const StepPages out = {C, pos, max_pos};
+        RT_TRY(step_base_case_mm(D, W, S, x_t, y_t, nullptr, nullptr, st, &out), "step_base_case_mm");
+        return RT_OK;
     }
-    RT_TRY(paged_finish_launch<T>(C, D, pos, max_pos, S.kv_raw, W.g_k, !mm && !D.norm_free, y_new, y_t, st), "paged_finish");
+    void *y_new = (char *)c->paged_slab + paged_rows_offset();
+    RT_TRY(paged_base_case_launch<T>(D, W, S, x_t, y_new, st), "paged_base_case");
+    RT_TRY(paged_finish_launch<T>(C, D, pos, max_pos, S.kv_raw, W.g_k, y_new, y_t, st), "paged_finish");
     return RT_OK;
 }
 

@@ -4,6 +4,7 @@
 #include <cstring>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include "rt_paged_index.h"
 
 namespace rt {
 
@@ -20,6 +21,8 @@ __device__ __forceinline__ bf16_t f32_to_bf16(float f)
     u += 0x7FFFu + ((u >> 16) & 1u);
     return (bf16_t)(u >> 16);
 }
+// the same for values that may be NaN (which stays NaN)
+__device__ __forceinline__ bf16_t f32_to_bf16_any(float f) { return f == f ? f32_to_bf16(f) : (bf16_t)0x7FC0; }
 __device__ __forceinline__ uint16_t f32_to_f16_bits(float f)
 {   // round to nearest, ties to even
     const _Float16 h = (_Float16)f;
@@ -34,6 +37,9 @@ __device__ __forceinline__ float to_f32(bf16_t v) { return bf16_to_f32(v); }
 template <typename T> __device__ __forceinline__ T from_f32(float f);
 template <> __device__ __forceinline__ float from_f32<float>(float f) { return f; }
 template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float f) { return f32_to_bf16(f); }
+template <typename T> __device__ __forceinline__ T from_f32_any(float f);   // values that may be NaN
+template <> __device__ __forceinline__ float from_f32_any<float>(float f) { return f; }
+template <> __device__ __forceinline__ bf16_t from_f32_any<bf16_t>(float f) { return f32_to_bf16_any(f); }
 
 // 8 consecutive elements -> 8 floats (16-byte aligned for bf16, 32-byte for f32)
 __device__ __forceinline__ void load8(const float *p, float *o)
@@ -256,8 +262,6 @@ template <typename T> struct Launch {
     // [Bc][Nc][d] tensor) -> Q, Kt, Vt rows ((n0 + n)*Bc + b)
     static hipError_t prepass(const LayerDims &D, const Weights &W, const Scratch &S, const void *x, int Bc, int Nc,
                               bool mfma, hipStream_t st, size_t x_bstride = 0, int n0 = 0, const PrepassPairs *pairs = nullptr);
-    // one position's raw [q | k_tmp | v_tmp] (decoding step) into S.qkv_raw
-    static hipError_t qkv_raw(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, size_t x_stride, hipStream_t st);
     // one position's q, k_tmp, v_tmp (decoding step): rows b of Q, Kt, Vt
     static hipError_t prepass_one(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, size_t x_stride,
                                   hipStream_t st, bool matrix_cores = false);
@@ -296,6 +300,7 @@ struct WaveLayer {
     const void *x;    // [B][N][d] input (the output of the layer below)
     void *y;          // [B][N][d] output
     void *K, *V;      // [kv_cap][B][H][64]
+    StepPages out;    // a step from pages: its pairs and its rows of y go here, by position
 };
 
 // Streams of the layer-wavefront engine: st[0] is the caller's, the others are lent to the call (default
@@ -325,7 +330,7 @@ bool step_uses_wide(const LayerDims &D);
 hipError_t step_qkv_wide(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, size_t x_stride, hipStream_t st);
 hipError_t step_qkv_mm(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, size_t x_stride, hipStream_t st);
 hipError_t step_base_case_mm(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, void *y_t, void *K_row,
-                             void *V_row, hipStream_t st);
+                             void *V_row, hipStream_t st, const StepPages *pages = nullptr);
 
 // Whole-sequence evaluation when every key-value pair is known in advance (rt_parallel.hip): the recompute of a
 // layer from its input and output (Sec. 6.1) and the standard Transformer layer (Sec. 2.1).  bf16 + matrix cores.

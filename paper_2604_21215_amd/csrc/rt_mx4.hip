@@ -158,22 +158,20 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
     };
     // loads come back in order: the first rows, then the matrix, which is on its way while the rows are split
     constexpr int kRaw = sizeof(T) / 2;   // 16-byte pieces of eight elements
-    uint4 znext[SL][4][kRaw], graw[SL][4][kRaw];
+    uint4 znext[4][kRaw], graw[SL][4][kRaw];
     const bool has_gain = PARTS == 2 || (PARTS == 3 && gain);
-    auto request_rows = [&](int c) {
+    auto request_rows = [&](int c, int s) {
         const T *zr = z + min(b0 + 16 * c + col, B - 1) * z_stride;   // columns beyond the batch repeat its last row (their results are dropped)
 #pragma unroll
-        for (int s = 0; s < SL; ++s)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int r = 0; r < kRaw; ++r) {
-                    const int k = min(blk[s], blocks - 1) * kMx4Block + 8 * j + r * (16 / (int)sizeof(T));
-                    znext[s][j][r] = *reinterpret_cast<const uint4 *>(zr + k);
-                    if (c == 0 && has_gain) graw[s][j][r] = *reinterpret_cast<const uint4 *>(gain + k);
-                }
+            for (int r = 0; r < kRaw; ++r) {
+                const int k = min(blk[s], blocks - 1) * kMx4Block + 8 * j + r * (16 / (int)sizeof(T));
+                znext[j][r] = *reinterpret_cast<const uint4 *>(zr + k);
+                if (c == 0 && has_gain) graw[s][j][r] = *reinterpret_cast<const uint4 *>(gain + k);
+            }
     };
-    request_rows(0);
+    request_rows(0, 0);
     __builtin_amdgcn_sched_barrier(0);
     int grp = blockIdx.x;
     request(grp);
@@ -182,26 +180,25 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
     Frag x[CT][SL][4][PARTS];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        uint4 zraw[SL][4][kRaw];
-#pragma unroll
-        for (int s = 0; s < SL; ++s)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int r = 0; r < kRaw; ++r) zraw[s][j][r] = znext[s][j][r];
-        if (c + 1 < CT) request_rows(c + 1);
         float ss = 0.f;
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
+            uint4 zraw[4][kRaw];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < kRaw; ++r) zraw[j][r] = znext[j][r];
+            if (s + 1 < SL) request_rows(c, s + 1);
+            else if (c + 1 < CT) request_rows(c + 1, 0);
             const bool in = blk[s] < blocks;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (!in) {   // past the row's end
 #pragma unroll
-                    for (int r = 0; r < kRaw; ++r) zraw[s][j][r] = make_uint4(0u, 0u, 0u, 0u);
+                    for (int r = 0; r < kRaw; ++r) zraw[j][r] = make_uint4(0u, 0u, 0u, 0u);
                 }
                 float v[8], gn[8];
-                eight(zraw[s][j], v);
+                eight(zraw[j], v);
                 if (has_gain) eight(graw[s][j], gn);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -209,7 +206,7 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
                     if (has_gain) v[e] *= gn[e];
                 }
                 if (PARTS == 1) {   // bf16 as it is
-                    x[c][s][j][0].u = zraw[s][j][0];
+                    x[c][s][j][0].u = zraw[j][0];
                     continue;
                 }
                 uint32_t p[8][PARTS];

@@ -5,15 +5,6 @@
 
 namespace rt {
 
-// A pool of pages as the kernels see it.
-struct PagedCache {
-    void *K, *V;              // [pages][H][page_len][64]: storage dtype, or int8 codes
-    uint8_t *Kx, *Vx;         // [pages][H][page_len] exponent bytes, or null
-    const int32_t *table;     // [S][table_stride]
-    long long table_stride;
-    int pages, lg;            // page_len = 2^lg
-};
-
 // Rows of cached pairs on the caller's side: row (s, n) starts s * seq_stride + n * pos_stride elements behind the pointer, heads contiguous.
 struct PairRows {
     const int32_t *first, *count;   // [S]: first position (negative: idle), rows (null: all N)
@@ -49,10 +40,14 @@ template <typename T> hipError_t cache_read_launch(const PagedCache &C, const Pa
 size_t paged_partials_bytes();
 void paged_partials(PagedAttention &A, void *slab);
 template <typename T> hipError_t paged_attention_launch(const PagedCache &C, const PagedAttention &A, hipStream_t st);
-// The last part of a paged step: the pairs of fp32 rows kv [S][2 d] (normalise: qkRMS of the key is still to be taken) into their pages
-// and the rows of y_new into y, for sequences that are not idle.
+// The last part of a paged step on the plain-ALU products: the pairs of fp32 rows kv [S][2 d] (raw) into their pages and the rows of y_new
+// into y, for sequences that are not idle.
 template <typename T>
 hipError_t paged_finish_launch(const PagedCache &C, const LayerDims &D, const int32_t *pos, int max_pos, const float *kv, const void *g_k,
-                               bool normalise, const void *y_new, void *y, hipStream_t st);
+                               const void *y_new, void *y, hipStream_t st);
+// The products of a step for the widths and types that step_mm_supported leaves out (rt_paged_products.hip).
+template <typename T> hipError_t paged_qkv_launch(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, hipStream_t st);
+template <typename T>
+hipError_t paged_base_case_launch(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, void *y_new, hipStream_t st);
 
 }  // namespace rt

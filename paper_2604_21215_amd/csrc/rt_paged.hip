@@ -52,12 +52,6 @@ __device__ __forceinline__ void widen(const uint4 &r, float (&f)[16], const int8
         for (int b = 0; b < 4; ++b) f[4 * e + b] = (float)(int8_t)(w[e] >> (8 * b));
 }
 
-// fp32 -> bf16 for values that may be infinite or NaN (a NaN stays one)
-__device__ __forceinline__ bf16_t f32_to_bf16_any(float f) { return f == f ? f32_to_bf16(f) : (bf16_t)0x7FC0; }
-template <typename T> __device__ __forceinline__ T from_f32_any(float f);
-template <> __device__ __forceinline__ float from_f32_any<float>(float f) { return f; }
-template <> __device__ __forceinline__ bf16_t from_f32_any<bf16_t>(float f) { return f32_to_bf16_any(f); }
-
 // ---------------------------------------------------------------- rows into pages and back
 // The position of row n of sequence s, or -1 where there is none: an idle sequence, a row past its count.  at_end: positions that the
 // sequence's line of the table has room for.
@@ -476,7 +470,7 @@ template <typename T> hipError_t paged_attention_launch(const PagedCache &C, con
 }
 
 // ---------------------------------------------------------------- the end of a paged step
-// One wavefront per (s, h): qkRMS of the key if it is still to be taken, the pair into its page row (rounded once from fp32, to the
+// One wavefront per (s, h): qkRMS of the key, the pair into its page row (rounded once from fp32, to the
 // storage dtype or to codes), and the head's slice of y.  grid (H, S), block 64.
 template <typename T>
 __global__ __launch_bounds__(64) void paged_finish_kernel(const PagedCache C, const int32_t *__restrict__ pos_of, int max_pos,
@@ -510,10 +504,10 @@ __global__ __launch_bounds__(64) void paged_finish_kernel(const PagedCache C, co
 }
 template <typename T>
 hipError_t paged_finish_launch(const PagedCache &C, const LayerDims &D, const int32_t *pos, int max_pos, const float *kv, const void *g_k,
-                               bool normalise, const void *y_new, void *y, hipStream_t st)
+                               const void *y_new, void *y, hipStream_t st)
 {
     hipLaunchKernelGGL(paged_finish_kernel<T>, dim3((unsigned)D.H, (unsigned)D.B), dim3(64), 0, st, C, pos, max_pos, kv, (const T *)g_k,
-                       normalise ? 1 : 0, D.H, D.eps, (const T *)y_new, (T *)y);
+                       !D.norm_free, D.H, D.eps, (const T *)y_new, (T *)y);
     return hipGetLastError();
 }
 
@@ -522,7 +516,7 @@ hipError_t paged_finish_launch(const PagedCache &C, const LayerDims &D, const in
     template hipError_t cache_read_launch<T>(const PagedCache &, const PairRows &, int, void *, void *, hipStream_t);            \
     template hipError_t paged_attention_launch<T>(const PagedCache &, const PagedAttention &, hipStream_t);                      \
     template hipError_t paged_finish_launch<T>(const PagedCache &, const LayerDims &, const int32_t *, int, const float *,       \
-                                               const void *, bool, const void *, void *, hipStream_t);
+                                               const void *, const void *, void *, hipStream_t);
 RT_PAGED_FOR(float)
 RT_PAGED_FOR(bf16_t)
 #undef RT_PAGED_FOR

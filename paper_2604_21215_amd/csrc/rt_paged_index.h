@@ -17,6 +17,22 @@ constexpr int kMinPage = 16, kMaxPage = 1024;   // positions of a page: a power 
 // Row (of 64 values) of position j of a page, head h, in a pool [pages][H][page_len][64] with page_len = 2^lg.
 RT_BOTH size_t pool_row(int page, int H, int h, int lg, int j) { return ((((size_t)page * (size_t)H) + (size_t)h) << lg) + (size_t)j; }
 
+// A pool of pages as the kernels see it.
+struct PagedCache {
+    void *K, *V;              // [pages][H][page_len][64]: storage dtype, or int8 codes
+    uint8_t *Kx, *Vx;         // [pages][H][page_len] exponent bytes, or null
+    const int32_t *table;     // [S][table_stride]
+    long long table_stride;
+    int pages, lg;            // page_len = 2^lg
+};
+
+// Where a decoding step caches its pairs instead of rows K, V: sequence s at position pos[s] (negative: idle, nothing is written for it).
+struct StepPages {
+    PagedCache C;
+    const int32_t *pos;   // null: no pages
+    int max_pos;
+};
+
 // A page table's entry is used only if it names a page of the pool.
 RT_BOTH bool page_ok(int entry, int pages) { return (uint32_t)entry < (uint32_t)pages; }
 

@@ -171,11 +171,55 @@ __device__ __forceinline__ float head_scale(const float *v, bool owner, bool liv
     return rsqrtf(((hss[col] + hss[ncol + col]) + (hss[2 * ncol + col] + hss[3 * ncol + col])) / (float)kHeadDim + eps);
 }
 
+// Four values (head dimensions 16 rg + 4 g ..) of the key or value row of sequence b, head h, into the row's page.  In 8 bits the largest value
+// of the row, whose parts lie in the four row groups and lane groups, meets in hss behind barriers that every wavefront reaches.
+__device__ __forceinline__ void page_store(const StepPages &out, const float *v, bool owner, bool live, int b, bool is_k, int h, int H, int g,
+                                           int rg, int col, int ncol, float *hss)
+{
+    const PagedCache &C = out.C;
+    uint32_t top = 0;
+    if (C.Kx) {
+        if (live) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = max(top, __float_as_uint(v[r]) & 0x7FFFFFFFu);
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+        __syncthreads();   // hss has been read (the head's scale)
+        if (owner && g == 0) hss[rg * ncol + col] = __uint_as_float(top);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(hss[i * ncol + col]));
+    }
+    if (!live) return;
+    const int pos = out.pos[b];
+    if (pos < 0 || pos > out.max_pos) return;
+    const int page = C.table[b * C.table_stride + (pos >> C.lg)];
+    if (!page_ok(page, C.pages)) return;
+    const size_t row = pool_row(page, H, h, C.lg, pos & ((1 << C.lg) - 1)), at = row * kHeadDim + 16 * rg + 4 * g;
+    void *dst = is_k ? C.K : C.V;
+    if (!C.Kx) {
+        *reinterpret_cast<uint2 *>((bf16_t *)dst + at) =
+            make_uint2((uint32_t)f32_to_bf16_any(v[0]) | (uint32_t)f32_to_bf16_any(v[1]) << 16,
+                       (uint32_t)f32_to_bf16_any(v[2]) | (uint32_t)f32_to_bf16_any(v[3]) << 16);
+        return;
+    }
+    const int byte = row_exponent(top);
+    const float inv = __uint_as_float(exponent_inverse_bits(byte));
+    uint32_t packed = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) packed |= (uint32_t)((byte == 255 ? 0 : (int)rintf(v[r] * inv)) & 255) << (8 * r);
+    *reinterpret_cast<uint32_t *>((int8_t *)dst + at) = packed;
+    if (rg == 0 && g == 0) (is_k ? C.Kx : C.Vx)[row] = (uint8_t)byte;
+}
+
 // What follows a finished 16 x 16 tile of one of the products: lane = outputs row0 + 4 g .. + 3 (g = lane / 16) of batch row b,
 // acc their sums, rscale the RMS scale of that row's input.  owner: this wavefront holds a tile; live: and b is a batch row.
 // rg, col: the tile's place in the workgroup, row group and batch column of ncol (EPI_KV: a workgroup is the head block_x of
 // [k heads | v heads], its four row groups meet in hss [4][ncol] behind a barrier that every wavefront reaches).
-template <int EPI>
+// PAGES (a decoding step): where Y.out has positions, the pair goes into its page (rounded once from fp32: to bf16 or to 8-bit codes) and y
+// is written for sequences that are not idle.
+template <int EPI, bool PAGES>
 __device__ __forceinline__ void mm_epilogue(const WaveLayer &Y, int t, const f32x4_t &acc, float rscale, bool owner, bool live, int b,
                                             int row0, int block_x, int rg, int col, int ncol, int B, int N, int d, int F, int H,
                                             float eps, int norm_free, float alpha, float *hss)
@@ -214,8 +258,9 @@ __device__ __forceinline__ void mm_epilogue(const WaveLayer &Y, int t, const f32
                 split_store4(Y.S.op_h, oo.x, oo.y, gv);
                 if (g == 0) Y.S.ssq_h[(size_t)b * (d / 16) + row0 / 16] = ss;
             } else {
-                *reinterpret_cast<uint2 *>((bf16_t *)Y.y + ((size_t)b * N + t) * d + o) =
-                    make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                if (!PAGES || !Y.out.pos || Y.out.pos[b] >= 0)
+                    *reinterpret_cast<uint2 *>((bf16_t *)Y.y + ((size_t)b * N + t) * d + o) =
+                        make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
                 split_store4(Y.S.op_z, oo.x, oo.y, gv);
                 if (g == 0) Y.S.ssq_z[(size_t)b * (d / 16) + row0 / 16] = ss;
             }
@@ -262,9 +307,8 @@ __device__ __forceinline__ void mm_epilogue(const WaveLayer &Y, int t, const f32
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] *= sc * (gk ? bf16_to_f32(gk[hh * kHeadDim + 16 * rg + 4 * g + r]) : 1.f);
         }
-        if (!Y.K) {   // the pair in fp32 rows [k | v] (a step from pages)
-            if (live)
-                *reinterpret_cast<float4 *>(Y.S.kv_raw + (size_t)b * 2 * d + hh * kHeadDim + 16 * rg + 4 * g) = make_float4(v[0], v[1], v[2], v[3]);
+        if (PAGES && Y.out.pos) {
+            page_store(Y.out, v, owner, live, b, is_k, is_k ? hh : hh - H, H, g, rg, col, ncol, hss);
             return;
         }
         if (live) {
@@ -429,7 +473,7 @@ __device__ __forceinline__ void mm_body(const WaveLayer &Y, int t, int block_x, 
         }
     }
     // wavefronts with kw == 0 hold the tile: lane = outputs (rows row0 + 4g .. + 3, batch row b0 + col)
-    mm_epilogue<EPI>(Y, t, acc, rscale, kw == 0, col < Bn && kw == 0, b0 + cb, row0, block_x, rg, col, kMmBatch, B, N, d, F, H, eps,
+    mm_epilogue<EPI, !PACKED>(Y, t, acc, rscale, kw == 0, col < Bn && kw == 0, b0 + cb, row0, block_x, rg, col, kMmBatch, B, N, d, F, H, eps,
                      norm_free, alpha, hss);
 }
 
@@ -568,7 +612,7 @@ __device__ __forceinline__ void wide_body(const WaveLayer &Y, int t, int block_x
 #pragma unroll
         for (int k = 0; k < kWideWaves - 1; ++k) sum += part[(wave * (kWideWaves - 1) + k) * 64 + lane];
     }
-    mm_epilogue<EPI>(Y, t, sum, rscale, owner, owner && b0 + col < B, cb, row0 + 16 * rg, block_x, rg, col, kWideBatch, B, N, d, F, H,
+    mm_epilogue<EPI, !PACKED>(Y, t, sum, rscale, owner, owner && b0 + col < B, cb, row0 + 16 * rg, block_x, rg, col, kWideBatch, B, N, d, F, H,
                      eps, norm_free, alpha, hss);
 }
 template <int EPI, int NO>
@@ -1042,6 +1086,7 @@ static WaveLayer step_layer(const Weights &W, const Scratch &S, const void *x_t,
     Y.S.Kh = nullptr;
     Y.S.VT = nullptr;
     Y.x = x_t; Y.y = y_t; Y.K = K_row; Y.V = V_row;
+    Y.out = StepPages{};
     return Y;
 }
 
@@ -1070,11 +1115,12 @@ hipError_t step_qkv_mm(const LayerDims &D, const Weights &W, const Scratch &S, c
 }
 
 // h = x_t + alpha Wo a (a as operand rows in S.op_a), MLP, y_t, and the persistent pair into K_row, V_row ([B][H][64]);
-// K_row null: in fp32 into S.kv_raw
+// or, given pages, into those, with y_t written for the sequences that are not idle
 hipError_t step_base_case_mm(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, void *y_t, void *K_row,
-                             void *V_row, hipStream_t st)
+                             void *V_row, hipStream_t st, const StepPages *pages)
 {
-    const WaveLayer Y = step_layer(W, S, x_t, y_t, K_row, V_row);
+    WaveLayer Y = step_layer(W, S, x_t, y_t, K_row, V_row);
+    if (pages) Y.out = *pages;
     hipError_t e;
     if (step_uses_wide(D)) {
         step_wide_launch<EPI_WO, 2>(Y, D.d, D, st);
