@@ -1378,7 +1378,7 @@ extern "C" rt_status rt_paged_attention(rt_ctx *c, const rt_paged_cache *cache, 
     A.q = q; A.kt = k_t; A.vt = v_t; A.q_stride = q_stride; A.kv_stride = kv_stride; A.out_stride = out_stride;
     A.out = out; A.lse = lse;
     paged_partials(A, c->paged_slab);
-    A.plan = split_plan(max_len, S, A.H);
+    A.plan = split_plan(max_len, S, A.H, cache->bits == 8);
     const PagedCache C = to_pool(*cache);
     const hipError_t e = c->cfg.dtype == RT_BF16 ? paged_attention_launch<bf16_t>(C, A, c->stream) : paged_attention_launch<float>(C, A, c->stream);
     if (e != hipSuccess) return fail_hip(c, e, "paged_attention");
@@ -1404,7 +1404,7 @@ static rt_status decode_paged(rt_ctx *c, LayerDims D, const rt_layer_weights *w,
     if (mm) { A.op_a = S.op_a; A.op_fragments = wide; }
     else A.attn_cat = S.attn_cat;
     paged_partials(A, c->paged_slab);
-    A.plan = split_plan(max_pos, D.B, D.H);
+    A.plan = split_plan(max_pos, D.B, D.H, C.Kx != nullptr);
     RT_TRY(paged_attention_launch<T>(C, A, st), "paged_attention");
     if (mm) {   // the products' own epilogues end the step
         const StepPages out = {C, pos, max_pos};

@@ -33,6 +33,21 @@ template <int LPR> __device__ __forceinline__ uint32_t row_max_bits(uint32_t v)
     return v;
 }
 
+// neighbours inside a row of 16 lanes, eight and four lanes on (every lane of the row gets the sum in the end)
+__device__ __forceinline__ float ror8(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xF, 0xF, true)); }
+__device__ __forceinline__ float ror4(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x124, 0xF, 0xF, true)); }
+// a summed over the lanes' halves in the low half (the even rows of 16), b in the high half (the odd rows)
+__device__ __forceinline__ float add_halves32(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add_halves16(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 __device__ __forceinline__ void widen(const uint4 &r, float (&f)[4], const float *)
 {
     f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y); f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
@@ -254,16 +269,16 @@ __device__ __forceinline__ void finish_row(const PagedAttention &A, int s, int h
 
 // C: type of the cached values (T or int8_t).  Workgroup = (h, s, split), heads first: consecutive workgroups go to different XCDs, and all
 // heads of a sequence have the same work, while the late splits of a ragged batch are mostly empty (splits first, and eight of them: an
-// XCD gets one split of every sequence, 512 pairs of up to 8000 positions: 125 us instead of 98).  Its four wavefronts share the split's rows in four runs.
+// XCD gets one split of every sequence, 512 pairs of up to 8000 positions: 125 us instead of 98).  Its wavefronts share the split's rows in as many runs.
 // A wavefront loads 64 rows of keys and of values (fp32: 32), or 16 where no more are left, before it computes on them.
-template <typename T, typename C, bool STEP>
-__global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P, const PagedAttention A)
+template <typename T, typename C, bool STEP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void paged_attention_kernel(const PagedCache P, const PagedAttention A)
 {
     constexpr int LPR = kLanesPerRow<C>, PL = kPerLane<C>, RPL = 64 / LPR, NL = sizeof(C) == 1 ? 4 : 8, CH = NL * RPL, SMALL = 16 / RPL;
     constexpr bool Q8 = sizeof(C) == 1;
-    __shared__ float sm[4 * RPL], sl[4 * RPL];
-    __shared__ float so[4 * RPL][kHeadDim];
-    __shared__ int sbad[4];
+    __shared__ float sm[WAVES], sl[WAVES];
+    __shared__ float so[WAVES][kHeadDim];
+    __shared__ int sbad[WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int split = blockIdx.z, h = blockIdx.x, s = blockIdx.y;
     const int lo = split * A.plan.split_len;
@@ -284,8 +299,8 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P
     if (lo >= n && !one) return;   // no rows here; the join counts the splits in the same way
     const int hi = min(n, lo + A.plan.split_len);
     // this wavefront's run: a quarter of the rows, in whole chunks where there is more than one for each
-    const int unit = hi - lo > 4 * 16 ? CH : 16;
-    const int share = ((hi - lo + 4 * unit - 1) / (4 * unit)) * unit;
+    const int unit = hi - lo > WAVES * 16 ? CH : 16;
+    const int share = ((hi - lo + WAVES * unit - 1) / (WAVES * unit)) * unit;
     const int wlo = lo + wave * share, whi = min(hi, wlo + share);
 
     const int c = lane % LPR, g = lane / LPR;
@@ -360,25 +375,45 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(const PagedCache P
         if (whi - r0 > 16) chunk(r0, std::integral_constant<int, NL>{});
         else chunk(r0, std::integral_constant<int, SMALL>{});
     }
-    // the groups' states meet in LDS
-    const int grp = wave * RPL + g;
-    if (c == 0) { sm[grp] = m; sl[grp] = l; }
-    if (lane == 0) sbad[wave] = bad;
-    __syncthreads();
-    float M = kLowest;
-    if (lane < 4 * RPL) M = sm[lane];
-    M = fast_max(M);
-    const float wgt = exp_diff(m, M);
+    // the groups' states meet inside the wavefront: their maximum, then the sums, each exchange halving what a lane holds of o
+    float mw = fmaxf(m, xor32(m));
+    mw = fmaxf(mw, xor16(mw));
+    if (LPR <= 8) mw = fmaxf(mw, ror8(mw));
+    if (LPR <= 4) mw = fmaxf(mw, ror4(mw));
+    const float wgt = exp_diff(m, mw);
+    l *= wgt;
+    l += xor32(l);
+    l += xor16(l);
+    if (LPR <= 8) l += ror8(l);
+    if (LPR <= 4) l += ror4(l);
 #pragma unroll
-    for (int e = 0; e < PL; ++e) so[grp][c * PL + e] = o[e] * wgt;
+    for (int e = 0; e < PL; ++e) o[e] *= wgt;
+#pragma unroll
+    for (int e = 0; e < PL / 2; ++e) o[e] = add_halves32(o[e], o[e + PL / 2]);
+#pragma unroll
+    for (int e = 0; e < PL / 4; ++e) {
+        o[e] = add_halves16(o[e], o[e + PL / 4]);
+        if (LPR <= 8) o[e] += ror8(o[e]);
+        if (LPR <= 4) o[e] += ror4(o[e]);
+    }
+    if ((lane & 15) < LPR) {
+        const int at = c * PL + (lane & 32 ? PL / 2 : 0) + (lane & 16 ? PL / 4 : 0);
+#pragma unroll
+        for (int e = 0; e < PL / 4; ++e) so[wave][at + e] = o[e];
+    }
+    if (lane == 0) { sm[wave] = mw; sl[wave] = l; sbad[wave] = bad; }
+    // the wavefronts' states in LDS
     __syncthreads();
     if (wave != 0) return;
-    float L = lane < 4 * RPL ? sl[lane] * exp_diff(sm[lane], M) : 0.f;
-    L = fast_sum(L);
+    float M = lane < WAVES ? sm[lane] : kLowest;
+    M = fast_max(M);
+    const float f = lane < WAVES ? exp_diff(sm[lane], M) : 0.f;
+    const float L0 = fast_sum(lane < WAVES ? sl[lane] * f : 0.f);
+    const bool any_bad = __any(lane < WAVES && sbad[lane]);
     float O = 0.f;
-#pragma unroll 16
-    for (int i = 0; i < 4 * RPL; ++i) O += so[i][lane];
-    const bool any_bad = sbad[0] | sbad[1] | sbad[2] | sbad[3];
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) O = fmaf(so[i][lane], lane_bcast(f, i), O);
+    float L = L0;
     if (one) {
         finish_row<T, STEP>(A, s, h, tok, M, L, O, any_bad);
         return;
@@ -455,11 +490,16 @@ void paged_partials(PagedAttention &A, void *slab)
     A.pl = A.pm + kMaxPartials;
 }
 
-template <typename T, bool STEP> static hipError_t attention_launch(const PagedCache &C, const PagedAttention &A, hipStream_t st)
+template <typename T, bool STEP, int WAVES> static void attention_go(const PagedCache &C, const PagedAttention &A, hipStream_t st)
 {
     const dim3 grid((unsigned)A.H, (unsigned)A.S, (unsigned)A.plan.n_splits);
-    if (C.Kx) hipLaunchKernelGGL((paged_attention_kernel<T, int8_t, STEP>), grid, dim3(256), 0, st, C, A);
-    else hipLaunchKernelGGL((paged_attention_kernel<T, T, STEP>), grid, dim3(256), 0, st, C, A);
+    if (C.Kx) hipLaunchKernelGGL((paged_attention_kernel<T, int8_t, STEP, WAVES>), grid, dim3(64 * WAVES), 0, st, C, A);
+    else hipLaunchKernelGGL((paged_attention_kernel<T, T, STEP, WAVES>), grid, dim3(64 * WAVES), 0, st, C, A);
+}
+template <typename T, bool STEP> static hipError_t attention_launch(const PagedCache &C, const PagedAttention &A, hipStream_t st)
+{
+    if (A.plan.waves == 16) attention_go<T, STEP, 16>(C, A, st);
+    else attention_go<T, STEP, 4>(C, A, st);
     if (A.plan.n_splits > 1)
         hipLaunchKernelGGL((paged_join_kernel<T, STEP>), dim3((unsigned)((A.S * A.H + 3) / 4)), dim3(256), 0, st, A);
     return hipGetLastError();

@@ -53,28 +53,39 @@ RT_BOTH int row_exponent(uint32_t top)
 RT_BOTH uint32_t exponent_step_bits(int byte) { return byte == 255 ? 0x7FC00000u : (uint32_t)byte << 23; }          // 2^e, 0 or NaN
 RT_BOTH uint32_t exponent_inverse_bits(int byte) { return byte == 0 || byte == 255 ? 0u : (uint32_t)(254 - byte) << 23; }   // 2^-e, or 0
 
-// How the positions below max_len of S sequences and H heads are cut: workgroups of split_len positions each (the last one shorter).
-// A cut costs a second launch and a stored state per part.  Few pairs of a sequence and a head are cut until the chip has something to do
-// (kWantGroups workgroups, parts of kShort positions and more); and all of them into parts of about kLong, which bounds how long one
-// sequence of a ragged batch keeps its workgroup after the others are done.  MI355X, us per call, S H pairs of up to so many positions, by
-// the number of parts (bf16):
-//   16 pairs, 700: one 7.3, three 7.8;  1000: one 8.8, four 7.6;  64 pairs, 2000: one 14.5, four 9.3, eight 8.5;
-//   256 pairs, 1000: one 10.9, four 11.6;  2000: one 20.3, three 17.6, eight 18.4;  8000: one 72.7, four 45.7, six 41.5, sixteen 41.8;
-//   512 pairs, 2000: one 27.9, two 30.4, eight 28.4;  8000: one 114, two 97.5, eight 98.0, 32 99.2;  1600 pairs, 8000 (8 bits): one 188,
-//   eight 160, 32 181;  32 pairs, 100001: one 1021, eight 154, 24 113, 98 122.
+// How the positions below max_len of S sequences and H heads are cut: workgroups of `waves` wavefronts and split_len positions each (the last
+// one shorter).  A cut costs a second launch and a stored state per part; a workgroup of sixteen wavefronts has as many loads on the way as four
+// of four and needs no second launch, but fills a compute unit by itself and idles where it has less than a chunk for each wavefront.
+//   Few pairs of a sequence and a head (at most kFewPairs), up to kWhole16 positions (up to kLong16 from half as many pairs on): sixteen
+//   wavefronts, one part.  Up to 256 positions four have enough to do.
+//   Else few pairs are cut until the chip has something to do (kWantGroups workgroups, parts of kShort positions and more), and all of them into
+//   parts of about kLong, which bounds how long one sequence of a ragged batch keeps its workgroup after the others are done.
+//   Many pairs, long rows in the storage dtype: sixteen wavefronts again, which end their sequences four times as early.
+// MI355X, us per call, S H pairs of up to so many positions, waves * parts (bf16 unless said):
+//   16 pairs, 500: 4*1 6.0, 16*1 5.6;  1000: 4*1 8.7, 4*4 7.7, 16*1 7.3;  2000: 4*1 14.3, 4*8 7.8, 16*1 10.5;  14 pairs, 513, fp32: 4*1 7.7, 16*1 5.8;
+//   64 pairs, 1000: 4*4 8.0, 16*1 7.3;  2000: 4*8 8.6, 16*1 10.6;  8000: 4*1 62, 4*16 17.6, 16*4 17.0;
+//   256 pairs, 500: 4*1 6.2, 16*1 5.9;  1000: 4*1 10.6, 16*1 8.1;  2000: 4*4 18.1, 16*1 14.8;  4000: 4*8 26.6, 16*1 24.0;  8000: 4*8 44, 16*1 44;
+//   512 pairs, 500: 4*1 9.8, 16*1 11.4;  2000: 4*1 27.8, 4*4 29.7, 16*1 26.3;  768 pairs, 1000: 4*1 20.1, 16*1 20.5;  4000: 4*4 76.8, 16*1 71.0;
+//   1024 pairs, 2000, 8 bits: 4*1 28.5, 16*1 33.3;  3200 pairs, 4096: 4*1 298, 4*4 294, 16*1 281;  8 bits: 4*1 184, 4*4 177, 16*1 193;
+//   1600 pairs, 8000, 8 bits: 4*1 188, 4*8 160, 16*1 176;  32 pairs, 100001: 4*1 1015, 4*8 152, 4*32 118, 4*64 117, 16*8 111.
 struct SplitPlan {
-    int split_len, n_splits;
+    int split_len, n_splits, waves;
 };
 constexpr int kMaxPartials = 65536;    // stored partial states of a call: S * H * n_splits if n_splits > 1
 constexpr int kSplitUnit = 256;        // four wavefronts of 64 positions
+constexpr int kFewPairs = 256, kWhole16 = 1280, kLong16 = 4096;
 constexpr int kWantGroups = 768, kShort = 256, kWhole = 640, kLong = 1024;
-RT_BOTH SplitPlan split_plan(int max_len, int S, int H)
+RT_BOTH SplitPlan split_plan(int max_len, int S, int H, bool eight_bits)
 {
     const int64_t pairs = (int64_t)S * H;
+    const bool few = pairs <= kFewPairs && max_len > 256 && max_len <= (2 * pairs > kFewPairs ? kLong16 : kWhole16);
+    const bool many = pairs > kFewPairs && !eight_bits && max_len >= kLong16 * 3 / 4;
     int64_t n = kWantGroups / pairs;
     const int64_t most = max_len <= kWhole ? 1 : (max_len + kShort - 1) / kShort;
     if (n > most) n = most;
     if (n < max_len / kLong) n = max_len / kLong;
+    if (few) n = 1;
+    if (many) n = max_len / (2 * kLong16);
     if (n > kMaxPartials / pairs) n = kMaxPartials / pairs;
     if (n < 1) n = 1;
     int64_t len = ((int64_t)max_len + n - 1) / n;
@@ -84,6 +95,7 @@ RT_BOTH SplitPlan split_plan(int max_len, int S, int H)
     p.split_len = (int)len;
     p.n_splits = (int)(((int64_t)max_len + len - 1) / len);
     if (p.n_splits < 1) p.n_splits = 1;
+    p.waves = few || many ? 16 : 4;
     return p;
 }
 

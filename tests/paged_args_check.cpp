@@ -60,8 +60,9 @@ static int plans()
     for (int len : lens)
         for (int S : seqs)
             for (int H : heads)
-                {
-                    const SplitPlan p = split_plan(len, S, H);
+                for (bool eight_bits : {false, true}) {
+                    const SplitPlan p = split_plan(len, S, H, eight_bits);
+                    EXPECT(p.waves == 4 || p.waves == 16);
                     EXPECT(p.n_splits >= 1 && p.split_len >= kSplitUnit && p.split_len % kSplitUnit == 0);
                     EXPECT((int64_t)p.n_splits * p.split_len >= len);
                     EXPECT(p.n_splits == 1 || (int64_t)(p.n_splits - 1) * p.split_len < len);

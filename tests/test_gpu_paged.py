@@ -52,7 +52,9 @@ ATTENTION = [("bf16", 0, 1, 1, 0, 16, 0.0, 1.0, True), ("bf16", 0, 1, 8, 1, 16, 
              ("bf16", 0, 9, 5, 300, 16, 8.0, 0.125, True), ("bf16", 8, 9, 5, 300, 16, 8.0, 0.125, True), ("f32", 0, 9, 3, 300, 32, 8.0, 0.125, True),
              ("f32", 8, 9, 3, 513, 64, 0.0, 0.125, False), ("bf16", 8, 3, 16, 2049, 256, 0.0, 1.0, True), ("bf16", 0, 3, 16, 2049, 1024, 8.0, 1.0, False),
              ("f32", 0, 2, 2, 5000, 16, 0.0, 1.0, True), ("bf16", 0, 2, 2, 20011, 64, 0.0, 0.125, True), ("bf16", 8, 2, 2, 20011, 128, 8.0, 0.125, True),
-             ("bf16", 8, 70, 2, 130, 32, 0.0, 1.0, True), ("f32", 0, 70, 1, 64, 16, 8.0, 1.0, False)]
+             ("bf16", 8, 70, 2, 130, 32, 0.0, 1.0, True), ("f32", 0, 70, 1, 64, 16, 8.0, 1.0, False), ("bf16", 0, 20, 8, 1500, 64, 8.0, 0.125, True),
+             ("bf16", 8, 20, 8, 1300, 16, 0.0, 0.125, False), ("f32", 0, 40, 4, 700, 32, 0.0, 0.125, True), ("bf16", 0, 150, 2, 3200, 128, 0.0, 0.125, True),
+             ("f32", 8, 3, 2, 1281, 16, 8.0, 0.125, True), ("bf16", 8, 2, 1, 257, 16, 0.0, 1.0, False)]
 
 
 @pytest.mark.parametrize("dtype,bits,S,H,most,page,alibi,scale,pair", ATTENTION)
