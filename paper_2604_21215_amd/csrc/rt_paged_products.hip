@@ -1,5 +1,5 @@
-// The matrix products of a decoding step from pages for widths that the stack engine's matrix-core products do not cover (d or d_hidden no
-// multiple of 256) and for fp32 layers: out[b][o] = epilogue(sum_k W[o][k] in[b][k]), every row of the batch in one launch.
+// The matrix products of a decoding step from pages for fp32 layers, for widths that the stack engine's matrix-core products do not cover (d
+// or d_hidden no multiple of 256), and for the batches in which they are the faster ones (paged_products_take): out[b][o] = epilogue(sum_k W[o][k] in[b][k]), every row of the batch in one launch.
 #include "rt_base_case.h"
 #include "rt_paged.h"
 #include "rt_ll.h"
@@ -89,15 +89,19 @@ __global__ __launch_bounds__(512) void paged_product_kernel(const T *__restrict_
     for (int t = 0; t < NO; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float ss = 0.f;
     const bool use_gain = do_norm && gain;
-    // two blocks at a time, both requested before the first is used; the second may lie past the end (zeros)
-    for (int k0 = 32 * wave; k0 < K; k0 += 2 * 32 * 8) {
+    // two blocks at a time, both requested before the first is used; the second may lie past the end (zeros).  Rows lie a power of two of
+    // bytes apart more often than not, so that the same block of all rows is behind one channel of the cache: every workgroup starts at
+    // another block (d = 1024, 16 rows: 50.7 -> 48.8 us for the whole step)
+    const int nblk = (K + 31) / 32, turn = (int)((blockIdx.x * 4 + blockIdx.y * 2) % (unsigned)nblk);
+    for (int j0 = wave; j0 < nblk; j0 += 2 * 8) {
         Side<T> s[2][NO];
         float v[2][8], gn[2][8];
         bool inside[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            inside[u] = k0 + 256 * u + 8 * g < K;   // K is a multiple of eight
-            const int k = inside[u] ? k0 + 256 * u + 8 * g : 0;
+            const int j = j0 + 8 * u, at = j + turn < nblk ? j + turn : j + turn - nblk;
+            inside[u] = j < nblk && 32 * at + 8 * g < K;   // K is a multiple of eight
+            const int k = inside[u] ? 32 * at + 8 * g : 0;
 #pragma unroll
             for (int t = 0; t < NO; ++t) s[u][t].load(w[t] + k, inside[u]);
             load8(x + k, v[u]);
@@ -167,6 +171,12 @@ static void product(const void *Wa, const void *Wb, const void *Wc, int n_first,
     else RT_PRODUCT(1);
 #undef RT_PRODUCT
 }
+
+// Where both kinds can run: these read the rows as fp32 and start 16 outputs by 16 rows at a time, the stack engine's prepare operand rows in
+// one product for the next.  MI355X, us per step (500 cached positions, bf16), these / the others: d = 1024, 1 row 39.1 / 35.2, 4 rows 41.3 / 42.5,
+// 8 43.9 / 51.1, 16 48.8 / 63.6, 32 56.8 / 76.1, 64 66.7 / 70.6, 128 101 / 82, 200 157 / 108;  d = 512, 1 row 28.6 / 28.1, 8 31.3 / 35.1, 32 36.1 / 45.6,
+// 128 51.5 / 57.2, 200 71.4 / 63.1;  d = 256, 4 rows 27.2 / 27.0, 16 30.4 / 33.4, 200 47.4 / 49.4.
+bool paged_products_take(const LayerDims &D) { return D.B >= 8 && (long long)D.B * D.d <= 65536; }
 
 // raw [q | k_tmp | v_tmp] of x_t [B][d] into S.qkv_raw
 template <typename T> hipError_t paged_qkv_launch(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, hipStream_t st)

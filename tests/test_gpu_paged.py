@@ -337,7 +337,8 @@ def _layer(seed, dtype, d, F):
 STEP = [("bf16", 0, 1, 256, 1024, 0, 16, 0.0, False), ("bf16", 0, 5, 256, 1024, 100, 16, 8.0, False), ("bf16", 8, 5, 512, 2048, 300, 32, 0.0, False),
         ("bf16", 8, 40, 512, 1024, 70, 16, 8.0, False), ("bf16", 0, 33, 512, 1536, 50, 16, 0.0, True), ("bf16", 8, 17, 256, 512, 600, 64, 0.0, True),
         ("bf16", 0, 4, 320, 640, 90, 16, 8.0, False), ("bf16", 8, 11, 192, 768, 90, 16, 0.0, False), ("f32", 0, 4, 128, 512, 130, 16, 8.0, False),
-        ("f32", 8, 9, 128, 264, 600, 32, 0.0, True)]
+        ("f32", 8, 9, 128, 264, 600, 32, 0.0, True), ("bf16", 8, 7, 256, 1024, 300, 16, 0.0, False), ("bf16", 8, 20, 256, 512, 40, 16, 8.0, False),
+        ("bf16", 8, 130, 512, 512, 30, 16, 0.0, False), ("bf16", 0, 140, 512, 2048, 20, 16, 8.0, False), ("bf16", 0, 30, 320, 264, 90, 16, 0.0, True)]
 
 
 @pytest.mark.parametrize("dtype,bits,S,d,F,most,page,alibi,norm_free", STEP)
