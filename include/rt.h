@@ -336,8 +336,10 @@ rt_status rt_paged_attention(rt_ctx *ctx, const rt_paged_cache *cache, int32_t S
  *   pos[s] < 0: an idle place: its row of y_t and its pages are left as they were (its row of x_t is read).  pos[s] > max_pos: its row of
  *   y_t is NaN, no page is written.
  *   Two sequences that share pages of earlier positions (a common prefix) are fine; row pos[s] must lie in a page of its own.
- *   x_t and y_t must not overlap each other or the cache.  1 <= S <= max_batch, 0 <= max_pos < min(2^20 + 1, table_stride * page_len).
- *   Ordinary launches (seven or eight): the products of rt_decode_step's launches between rt_paged_attention's kernels.  q and the temporary pair stay in fp32.
+ *   x_t and y_t lie on 16 bytes and must not overlap each other or the cache.  1 <= S <= max_batch, 0 <= max_pos < min(2^20 + 1,
+ *   table_stride * page_len).
+ *   Six to eight ordinary launches: rt_paged_attention's kernels between the five products, on the matrix cores (with RT_FLAG_NO_MFMA on the
+ *   plain ALUs, eight rows a launch).  q and the temporary pair stay in fp32; bf16 products take each vector as head and remainder.
  *   Scratch, capture: as rt_paged_attention. */
 rt_status rt_decode_step_paged(rt_ctx *ctx, const rt_layer_weights *w, const rt_paged_cache *cache, const void *x_t, int32_t S,
                                const int32_t *pos, int32_t max_pos, void *y_t);

@@ -1394,8 +1394,10 @@ static rt_status decode_paged(rt_ctx *c, LayerDims D, const rt_layer_weights *w,
     Scratch S = c->S;
     S.Q = nullptr;   // the queries and the temporary pairs stay in fp32 rows
     const bool mm = sizeof(T) == 2 && step_mm_supported(D, c->use_mfma) && !paged_products_take(D), wide = mm && step_uses_wide(D);
+    const bool alus = (c->cfg.flags & RT_FLAG_NO_MFMA) != 0;
     if (wide) RT_TRY(step_qkv_wide(D, W, S, x_t, (size_t)D.d, st), "step_qkv_wide");
     else if (mm) RT_TRY(step_qkv_mm(D, W, S, x_t, (size_t)D.d, st), "step_qkv_mm");
+    else if (alus) RT_TRY(Launch<T>::qkv_raw(D, W, S, x_t, (size_t)D.d, st), "qkv_raw");
     else RT_TRY(paged_qkv_launch<T>(D, W, S, x_t, st), "paged_qkv");
     PagedAttention A = {};
     A.S = D.B; A.H = D.H; A.max_len = max_pos; A.lens = pos;
@@ -1412,7 +1414,14 @@ static rt_status decode_paged(rt_ctx *c, LayerDims D, const rt_layer_weights *w,
         return RT_OK;
     }
     void *y_new = (char *)c->paged_slab + paged_rows_offset();
-    RT_TRY(paged_base_case_launch<T>(D, W, S, x_t, y_new, st), "paged_base_case");
+    if (alus) {
+        RT_TRY(Launch<T>::gemv_wo(D, W, S, x_t, (size_t)D.d, st), "gemv_wo");
+        RT_TRY(Launch<T>::gemv_w1(D, W, S, st), "gemv_w1");
+        RT_TRY(Launch<T>::gemv_w2(D, W, S, y_new, (size_t)D.d, st), "gemv_w2");
+        RT_TRY(Launch<T>::gemv_kv(D, W, S, st), "gemv_kv");
+    } else {
+        RT_TRY(paged_base_case_launch<T>(D, W, S, x_t, y_new, st), "paged_base_case");
+    }
     RT_TRY(paged_finish_launch<T>(C, D, pos, max_pos, S.kv_raw, W.g_k, y_new, y_t, st), "paged_finish");
     return RT_OK;
 }

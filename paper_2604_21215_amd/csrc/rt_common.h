@@ -262,6 +262,8 @@ template <typename T> struct Launch {
     // [Bc][Nc][d] tensor) -> Q, Kt, Vt rows ((n0 + n)*Bc + b)
     static hipError_t prepass(const LayerDims &D, const Weights &W, const Scratch &S, const void *x, int Bc, int Nc,
                               bool mfma, hipStream_t st, size_t x_bstride = 0, int n0 = 0, const PrepassPairs *pairs = nullptr);
+    // one position's raw [q | k_tmp | v_tmp] (decoding step) into S.qkv_raw
+    static hipError_t qkv_raw(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, size_t x_stride, hipStream_t st);
     // one position's q, k_tmp, v_tmp (decoding step): rows b of Q, Kt, Vt
     static hipError_t prepass_one(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, size_t x_stride,
                                   hipStream_t st, bool matrix_cores = false);

@@ -130,6 +130,8 @@ inline rt_status check_paged_step(const rt_config &cfg, const rt_paged_cache *ca
     if (S > cfg.max_batch) return RT_ERR_INVALID_ARG;
     *msg = "max_pos out of range [0, min(2^20, table_stride page_len - 1)]";
     if (max_pos < 0 || max_pos > (1 << 20) || max_pos >= cache->table_stride * cache->page_len) return RT_ERR_INVALID_ARG;
+    *msg = "x_t and y_t must lie on 16 bytes";
+    if (!on16(x_t) || !on16(y_t)) return RT_ERR_INVALID_ARG;
     const size_t bytes = (size_t)S * (size_t)cfg.d_model * (size_t)storage_bytes(cfg);
     const ByteRange x = {x_t, bytes}, y = {y_t, bytes};
     *msg = "the cache, x_t, y_t must not overlap";

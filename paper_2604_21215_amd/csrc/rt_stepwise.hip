@@ -395,6 +395,14 @@ static hipError_t gemv_launch(const T *Wa, const T *Wb, const T *Wc, int n_first
     return hipGetLastError();
 }
 
+template <typename T>
+hipError_t Launch<T>::qkv_raw(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, size_t x_stride, hipStream_t st)
+{
+    return gemv_launch<T, T, EPI_KV>((const T *)W.Wq, (const T *)W.Wk, (const T *)W.Wv, D.d, 3 * D.d, D.d, (const T *)x_t, x_stride, D.B,
+                                     (const T *)W.g_attn, D.eps, D.norm_free ? 0 : 1, D.alpha, (const T *)nullptr, (size_t)0,
+                                     (const float *)nullptr, S.qkv_raw, (T *)nullptr, (size_t)0, st);
+}
+
 // One position's [q | k_tmp | v_tmp] (a decoding step): the three products as one small-M launch, then the per-head
 // normalisation.  x_t rows are B apart by x_stride elements.
 template <typename T>
@@ -402,10 +410,7 @@ hipError_t Launch<T>::prepass_one(const LayerDims &D, const Weights &W, const Sc
                                   hipStream_t st, bool matrix_cores)
 {
     if (matrix_cores && step_uses_wide(D)) return step_qkv_wide(D, W, S, x_t, x_stride, st);
-    hipError_t e = matrix_cores ? step_qkv_mm(D, W, S, x_t, x_stride, st) : gemv_launch<T, T, EPI_KV>((const T *)W.Wq, (const T *)W.Wk, (const T *)W.Wv, D.d, 3 * D.d, D.d,
-                                             (const T *)x_t, x_stride, D.B, (const T *)W.g_attn, D.eps, D.norm_free ? 0 : 1,
-                                             D.alpha, (const T *)nullptr, (size_t)0, (const float *)nullptr, S.qkv_raw,
-                                             (T *)nullptr, (size_t)0, st);
+    hipError_t e = matrix_cores ? step_qkv_mm(D, W, S, x_t, x_stride, st) : qkv_raw(D, W, S, x_t, x_stride, st);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(finalize_qkv_kernel<T>, dim3(D.B * D.H), dim3(64), 0, st, S.qkv_raw, (const T *)W.g_q, (const T *)W.g_k,
                        (T *)S.Q, (T *)S.Kt, (T *)S.Vt, D.H, D.d, D.eps, D.norm_free);

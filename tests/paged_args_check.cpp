@@ -143,6 +143,7 @@ static int refusals()
     auto step = [&](void *x, int S, const int32_t *pos, int most, void *y) { return check_paged_step(cfg, &p, R, x, S, pos, most, y, &msg); };
     EXPECT(step(q, 8, ints, 319, out) == RT_OK && step(q, 8, ints, 320, out) == RT_ERR_INVALID_ARG && step(q, 8, ints, -1, out) == RT_ERR_INVALID_ARG);
     EXPECT(step(q, 9, ints, 5, out) == RT_ERR_INVALID_ARG && step(q, 8, nullptr, 5, out) == RT_ERR_INVALID_ARG && step(q, 8, ints, 5, q + 512) == RT_ERR_INVALID_ARG);
+    EXPECT(step(q + 8, 8, ints, 5, out) == RT_ERR_INVALID_ARG && step(q, 8, ints, 5, out + 8) == RT_ERR_INVALID_ARG);
     EXPECT(step(at(1ull << 40), 8, ints, 5, out) == RT_ERR_INVALID_ARG && step(q, 8, ints, 5, nullptr) == RT_ERR_INVALID_ARG);
 
     const uint8_t *codes = (const uint8_t *)at(12ull << 40), *exps = (const uint8_t *)at(13ull << 40);

@@ -115,3 +115,37 @@ def test_rows_that_are_not_finite():
         want = z[2, 1].astype(np.float64) @ mx4_values(codes, exps).T      # an infinity with its weight's sign, NaN where the weight is 0
     np.testing.assert_array_equal(np.isnan(free[2]), np.isnan(want))
     np.testing.assert_array_equal(np.sign(free[2][~np.isnan(want)]), np.sign(want[~np.isnan(want)]))
+
+
+@pytest.mark.parametrize("dtype,d,B", [("bf16", 1024, 1), ("bf16", 512, 64), ("f32", 4224, 2)])
+def test_captured(dtype, d, B):
+    """A captured read-out, replayed on other rows among eager calls: every replay gives the eager call's bits."""
+    from paper_2604_21215_amd import binding, torch_io as tio
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible")
+    rng = np.random.default_rng(d)
+    codes, exps = (torch.from_numpy(a).to("cuda:0") for a in binding.rt_mx4_pack((rng.standard_normal((500, d)) * 0.05).astype(np.float32)))
+    st = torch.cuda.Stream()
+    ctx = binding.RTContext(d, d // 64, 64, B, 1, dtype, rms_eps=1e-6, stream=st.cuda_stream)
+    try:
+        z, g = torch.zeros((B, d), dtype=tio.torch_dtype(dtype), device="cuda:0"), torch.ones(d, dtype=tio.torch_dtype(dtype), device="cuda:0")
+        out = torch.zeros((B, 500), device="cuda:0")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            ctx.rt_lm_head_mx4(codes, exps, g, z, d, B, out)
+        for rep in range(3):
+            z.copy_(torch.randn((B, d), device="cuda:0"))
+            torch.cuda.synchronize()
+            with torch.cuda.stream(st):
+                ctx.rt_lm_head_mx4(codes, exps, g, z, d, B, out)
+            torch.cuda.synchronize()
+            eager = out.clone()
+            out.zero_()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(st):
+                graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, eager) and float(out.abs().max()) > 0
+    finally:
+        ctx.rt_destroy()

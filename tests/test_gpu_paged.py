@@ -388,6 +388,33 @@ def test_decode_step_from_pages(dtype, bits, S, d, F, most, page, alibi, norm_fr
         np.testing.assert_array_equal(a[~touched], b[~touched])
 
 
+@pytest.mark.parametrize("dtype,d,S", [("bf16", 256, 3), ("bf16", 256, 20), ("f32", 192, 11), ("bf16", 512, 40)])
+def test_step_on_the_plain_alus_agrees(dtype, d, S):
+    """RT_FLAG_NO_MFMA: the same step on other kernels.  Both are within the tolerance of the float64 layer, so within twice of each other; the
+    cached pairs of bf16 differ by a rounding where the sums fall on either side."""
+    from paper_2604_21215_amd import binding, torch_io as tio
+    from tests.parity_util import TOL
+    H, pos = d // 64, _lens(np.random.default_rng(S), S, 100)
+    w, g = _layer(12, dtype, d, 4 * d)
+    dl = tio.DeviceLayer(w, g, dtype)
+    x = tio.to_device(_rows(np.random.default_rng(1), dtype, S, d), dtype)
+    got = []
+    for flags in (0, binding.RT_FLAG_NO_MFMA):
+        pool = ref.Pool(np.random.default_rng(d), dtype, 0, S, H, pos, 16, room=1)
+        ctx = _context(d, S, dtype, attn_scale=0.125, flags=flags)
+        try:
+            y = torch.zeros_like(x)
+            ctx.rt_decode_step_paged(dl.struct, pool.cache(), x, _ints(pos), 100, y)
+            ko, vo = (torch.zeros((S, 1, H, 64), dtype=x.dtype, device="cuda:0") for _ in range(2))
+            ctx.rt_cache_read(pool.cache(), _ints(pos), None, ko, vo)
+            torch.cuda.synchronize()
+            got.append([_host(t) for t in (y, ko, vo)])
+        finally:
+            ctx.rt_destroy()
+    for a, b in zip(*got):
+        assert np.linalg.norm(a - b) <= 2 * TOL[dtype] * np.linalg.norm(b) and np.linalg.norm(b) > 0
+
+
 def test_step_beyond_its_bound_and_without_a_page():
     """pos > max_pos: y is NaN and nothing is cached; a wrong page for the new row: y as ever, nothing cached."""
     from paper_2604_21215_amd import torch_io as tio
