@@ -116,22 +116,25 @@ __device__ __forceinline__ void eight(const uint4 (&r)[2], float (&f)[8])
     for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(w[e]);
 }
 
-// The rows stay in registers and the matrix streams past them.  A workgroup has a wavefront per slice of 128 indices (up to 8, each with SL
+// The rows stay in registers and the matrix streams past them.  A workgroup has a wavefront per slice of 128 indices (up to WMAX, each with SL
 // slices): it holds the fragments of its slices for 16 CT batch rows, made from z once, and per tile of 16 vocabulary rows loads 16 bytes per
 // lane and slice, turns them into four fragments and feeds 4 CT PARTS matrix instructions.  The slices' partial tiles meet in LDS, RT tiles at
 // a time, and are summed in slice order; the row's 1 / rms is applied to the sum.  No element of z is read or split twice by a workgroup, and
 // nothing but partial tiles goes through LDS.
-// Bound: for few rows the matrix (17 bytes per 32 weights); from some 64 rows on the matrix instructions.
+// Bound: for few rows the matrix (17 bytes per 32 weights; one row, d = 1024, 32768 vocabulary rows: 7.8 us = 2.3 TB/s, of which some 4 us are
+// the launch and the first trip to memory); for 64 rows the chain of loads, conversions, products and sums that the two wavefronts of a SIMD
+// walk through (50001 vocabulary rows: 23.7 us; with rows staged in LDS and the matrix read once per 16 rows 187).
+// 32 columns and twice the wavefronts: 32 us; two tiles per barrier at 64 columns: 24.6.
 // grid (<= groups of RT tiles, batch tiles of 16 CT), block 64 NW.
-template <typename T, int PARTS, int CT, int SL, int RT>
-__global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ exps,
+template <typename T, int PARTS, int CT, int SL, int RT, int WMAX>
+__global__ __launch_bounds__(64 * WMAX) void mx4_rows_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ exps,
                                                        const T *__restrict__ gain, const T *__restrict__ z, long long z_stride,
                                                        float *__restrict__ logits, int B, int d, int vocab, float eps, int norm_free)
 {
     extern __shared__ __align__(16) unsigned char mx_smem[];
     const int NW = blockDim.x >> 6;
-    float *ssq = reinterpret_cast<float *>(mx_smem);                                 // [8][16 CT] sums of squares, slice by slice
-    f32x4_t *part = reinterpret_cast<f32x4_t *>(mx_smem + 9 * 16 * CT * 4);          // [2][RT][NW][16 CT][4]
+    float *ssq = reinterpret_cast<float *>(mx_smem);                                 // [WMAX][16 CT] sums of squares, slice by slice
+    f32x4_t *part = reinterpret_cast<f32x4_t *>(mx_smem + (WMAX + 1) * 16 * CT * 4);          // [2][RT][NW][16 CT][4]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int b0 = blockIdx.y * 16 * CT, blocks = d / kMx4Block;
@@ -226,7 +229,7 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
         if (g == 0) ssq[wave * 16 * CT + 16 * c + col] = ss;
     }
     __syncthreads();
-    float *rinv = ssq + 8 * 16 * CT;   // [16 CT]
+    float *rinv = ssq + WMAX * 16 * CT;   // [16 CT]
     if (threadIdx.x < 16 * CT) {
         float ss = 0.f;
         for (int w = 0; w < NW; ++w) ss += ssq[w * 16 * CT + threadIdx.x];
@@ -239,13 +242,17 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
             const int v = group * RT * 16 + o % (16 * RT), t = (o >> 4) % RT, q = o / (16 * RT);
             if (b0 + 4 * q >= B || v >= vocab) continue;
             const f32x4_t *p = src + (t * NW * 4 * CT + q) * 16 + (o & 15);
-            f32x4_t s[8];
+            f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < 8; ++w) s[w] = p[min(w, NW - 1) * 4 * CT * 16];   // all on the way before the first is added
-            f32x4_t sum = s[0];
+            for (int w0 = 0; w0 < WMAX; w0 += 8) {
+                if (w0 >= NW) break;
+                f32x4_t s[8];
 #pragma unroll
-            for (int w = 1; w < 8; ++w)
-                if (w < NW) sum += s[w];
+                for (int w = 0; w < 8; ++w) s[w] = p[min(w0 + w, NW - 1) * 4 * CT * 16];   // eight on the way before the first is added
+#pragma unroll
+                for (int w = 0; w < 8; ++w)
+                    if (w0 + w < NW) sum += s[w];
+            }
             float *out = logits + (size_t)(b0 + 4 * q) * vocab + v;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
@@ -254,7 +261,7 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
     };
     // Half of the wavefronts finish the group before while the other half, on the same SIMDs, keep the matrix units busy, and the other way
     // round: one barrier per group, partial tiles in two halves.
-    const bool early = wave < 4;
+    const bool early = (wave & 4) == 0;
     int last = -1;
     for (int buf = 0; grp < groups; buf ^= 1) {
         f32x4_t *dst = part + buf * RT * NW * 16 * CT * 4, *prev = part + (buf ^ 1) * RT * NW * 16 * CT * 4;
@@ -266,32 +273,49 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
             for (int s = 0; s < SL; ++s) { wc[t][s] = nc[t][s]; we[t][s] = ne[t][s]; }
         if (grp < groups) request(grp);   // a whole group ahead
         if (early && last >= 0) finish(prev, last);
+        // the fragments of one slice of one tile ahead of the products: the conversions take a fourth of the vector rate, and the matrix
+        // units have work meanwhile
+        Frag a[2][4];
+        unsigned long long odd[RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            f32x4_t acc[CT];
+        for (int t = 0; t < RT; ++t) odd[t] = 0;
+        auto convert = [&](Frag(&f)[4], int u) {   // past a row's end the rows' fragments are zero: any block of the row will do
+            const uint4 c4 = wc[u / SL][u % SL];
+            const int byte = we[u / SL][u % SL];
+            const float scale = __uint_as_float((uint32_t)byte << 23);
+            f[0] = weight_fragment(c4.x, scale);
+            f[1] = weight_fragment(c4.y, scale);
+            f[2] = weight_fragment(c4.z, scale);
+            f[3] = weight_fragment(c4.w, scale);
+            odd[u / SL] |= __ballot(byte == 0 || byte == 255);   // no scale: the row's logits are NaN
+        };
+        convert(a[0], 0);
+        f32x4_t acc[CT];
 #pragma unroll
-            for (int c = 0; c < CT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int u = 0; u < RT * SL; ++u) {
+            const int t = u / SL, s = u % SL;
+            if (u + 1 < RT * SL) convert(a[(u + 1) & 1], u + 1);
+            if (s == 0) {
 #pragma unroll
-            for (int s = 0; s < SL; ++s) {
-                const float scale = __uint_as_float((uint32_t)we[t][s] << 23);
-                const bool in = blk[s] < blocks, odd = in && (we[t][s] == 0 || we[t][s] == 255);   // odd: no scale, the block reads as NaN
-                const uint32_t cw[4] = {wc[t][s].x, wc[t][s].y, wc[t][s].z, wc[t][s].w};
-                Frag a[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    a[j] = weight_fragment(in ? cw[j] : 0u, in ? scale : 1.f);
-                    if (odd) a[j].u = make_uint4(0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u);
-                }
-#pragma unroll
-                for (int i = PARTS - 1; i >= 0; --i)   // the smallest part first
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int c = 0; c < CT; ++c) acc[c] = mfma16(x[c][s][j][i], a[j], acc[c]);
+                for (int c = 0; c < CT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
 #pragma unroll
-            for (int c = 0; c < CT; ++c) dst[((t * NW + wave) * 4 * CT + 4 * c + g) * 16 + col] = acc[c];   // batch rows 4 g .., vocabulary row col
-            __builtin_amdgcn_sched_barrier(0);   // tile by tile, for the same reason
+            for (int i = PARTS - 1; i >= 0; --i)   // the smallest part first
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) acc[c] = mfma16(x[c][s][j][i], a[u & 1][j], acc[c]);
+            if (s == SL - 1) {
+                if (odd[t]) {
+                    const unsigned long long rows = odd[t] | odd[t] >> 16 | odd[t] >> 32 | odd[t] >> 48;
+                    if (rows >> col & 1) {
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) acc[c] = f32x4_t{} + __uint_as_float(0x7FC00000u);
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < CT; ++c) dst[((t * NW + wave) * 4 * CT + 4 * c + g) * 16 + col] = acc[c];   // batch rows 4 g .., vocabulary row col
+            }
         }
         if (!early && last >= 0) finish(prev, last);
         last = now;
@@ -300,17 +324,17 @@ __global__ __launch_bounds__(512) void mx4_rows_kernel(const uint8_t *__restrict
     }
 }
 
-template <typename T, int PARTS, int CT, int SL, int RT>
+template <typename T, int PARTS, int CT, int SL, int RT, int WMAX>
 static hipError_t mx4_rows_go(const uint8_t *codes, const uint8_t *exps, const T *g, const T *z, long long z_stride, float *logits, int B, int d,
                               int vocab, float eps, int norm_free, hipStream_t st)
 {
     const int slices = (d + 127) / 128, NW = (slices + SL - 1) / SL;
-    const size_t lds = 9 * 16 * CT * 4 + (size_t)2 * RT * NW * 16 * CT * 16 * 4;
-    const hipError_t e = hipFuncSetAttribute((const void *)mx4_rows_kernel<T, PARTS, CT, SL, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    const size_t lds = (WMAX + 1) * 16 * CT * 4 + (size_t)2 * RT * NW * 16 * CT * 16 * 4;
+    const hipError_t e = hipFuncSetAttribute((const void *)mx4_rows_kernel<T, PARTS, CT, SL, RT, WMAX>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (e != hipSuccess) return e;
     const int groups = (vocab + 16 * RT - 1) / (16 * RT), chunks = (B + 16 * CT - 1) / (16 * CT);
     const int most = CT >= 4 ? 256 : 512;
-    hipLaunchKernelGGL((mx4_rows_kernel<T, PARTS, CT, SL, RT>), dim3(groups < most ? groups : most, chunks), dim3(64 * NW), lds, st, codes, exps, g, z,
+    hipLaunchKernelGGL((mx4_rows_kernel<T, PARTS, CT, SL, RT, WMAX>), dim3(groups < most ? groups : most, chunks), dim3(64 * NW), lds, st, codes, exps, g, z,
                        z_stride, logits, B, d, vocab, eps, norm_free);
     return hipGetLastError();
 }
@@ -395,23 +419,24 @@ hipError_t mx4_head_launch(const uint8_t *codes, const uint8_t *exps, const void
                            int d, int vocab, float eps, int norm_free, hipStream_t st)
 {
     const T *gt = norm_free ? nullptr : (const T *)g, *zt = (const T *)z;
-#define RT_MX4_GO(PARTS, CT, SL, RT_) return mx4_rows_go<T, PARTS, CT, SL, RT_>(codes, exps, gt, zt, z_stride, logits, B, d, vocab, eps, norm_free, st)
+#define RT_MX4_GO(PARTS, CT, SL, RT_, WMAX) \
+    return mx4_rows_go<T, PARTS, CT, SL, RT_, WMAX>(codes, exps, gt, zt, z_stride, logits, B, d, vocab, eps, norm_free, st)
     // the rows' 16-byte loads: anything else goes the way of the wide rows
     const bool wide = d > 4096 || (z_stride * (long long)sizeof(T)) % 16 != 0 || ((uintptr_t)z & 15) != 0 || ((uintptr_t)g & 15) != 0;
     if (wide) {
     } else if constexpr (sizeof(T) == 2) {
         if (gt) {
-            if (d <= 1024) { if (B <= 16) RT_MX4_GO(2, 1, 1, 4); if (B <= 32) RT_MX4_GO(2, 2, 1, 2); RT_MX4_GO(2, 4, 1, 2); }
-            if (d <= 2048) { if (B <= 16) RT_MX4_GO(2, 1, 2, 2); RT_MX4_GO(2, 2, 2, 2); }
-            RT_MX4_GO(2, 1, 4, 1);
+            if (d <= 1024) { if (B <= 16) RT_MX4_GO(2, 1, 1, 4, 8); if (B <= 32) RT_MX4_GO(2, 2, 1, 2, 8); RT_MX4_GO(2, 4, 1, 1, 8); }
+            if (d <= 2048) { if (B <= 16) RT_MX4_GO(2, 1, 1, 2, 16); RT_MX4_GO(2, 2, 1, 1, 16); }
+            RT_MX4_GO(2, 1, 2, 1, 16);
         } else {
-            if (d <= 1024) { if (B <= 16) RT_MX4_GO(1, 1, 1, 4); if (B <= 32) RT_MX4_GO(1, 2, 1, 2); RT_MX4_GO(1, 4, 1, 2); }
-            if (d <= 2048) { if (B <= 16) RT_MX4_GO(1, 1, 2, 2); RT_MX4_GO(1, 2, 2, 2); }
-            RT_MX4_GO(1, 1, 4, 1);
+            if (d <= 1024) { if (B <= 16) RT_MX4_GO(1, 1, 1, 4, 8); if (B <= 32) RT_MX4_GO(1, 2, 1, 2, 8); RT_MX4_GO(1, 4, 1, 1, 8); }
+            if (d <= 2048) { if (B <= 16) RT_MX4_GO(1, 1, 1, 2, 16); RT_MX4_GO(1, 2, 1, 1, 16); }
+            RT_MX4_GO(1, 1, 2, 1, 16);
         }
     } else {
-        if (d <= 1024) { if (B <= 16) RT_MX4_GO(3, 1, 1, 4); RT_MX4_GO(3, 2, 1, 2); }
-        if (d <= 2048) RT_MX4_GO(3, 1, 2, 2);
+        if (d <= 1024) { if (B <= 16) RT_MX4_GO(3, 1, 1, 4, 8); RT_MX4_GO(3, 2, 1, 2, 8); }
+        if (d <= 2048) RT_MX4_GO(3, 1, 1, 1, 16);
     }
 #undef RT_MX4_GO
     int bt = (int)(kMxMaxLds / ((size_t)3 * mx_ld(d) * 2));
