@@ -1,7 +1,8 @@
 """Pages of a stack's key-value caches: the pools of all layers, one page table, and which pages are free.
 
 A sequence has a place (a row of the table).  Pages are given out on the host, one number for the same page of every layer's pool; the
-rows in them are written and read by the library's kernels only."""
+rows in them are written and read by the library's kernels only.  reserve and release copy the table to the device on torch's current
+stream: that is the stream of the context that reads it, or one that the caller orders with it."""
 from __future__ import annotations
 
 import torch
@@ -32,11 +33,14 @@ class PagedCaches:
         self.layer = [binding.make_cache(self.K[l], self.V[l], self.table, self.K_exp[l], self.V_exp[l]) for l in range(layers)]
 
     def reserve(self, lengths) -> None:
-        """Pages for positions 0 .. lengths[s] - 1 of every place s (a length below what a place holds changes nothing).  Raises before
-        anything is given out if there are not enough."""
-        need = [max(0, -(-int(n) // self.page_len) - self.held[s]) for s, n in enumerate(lengths)]
-        if any(int(n) > self.max_len for n in lengths):
+        """Pages for positions 0 .. lengths[s] - 1 of every place s (a length below what a place holds changes nothing; places past the
+        last length keep what they hold).  Raises before anything is given out if there are not enough."""
+        lengths = [int(n) for n in lengths]
+        if len(lengths) > len(self.held):
+            raise ValueError("%d lengths for %d places" % (len(lengths), len(self.held)))
+        if any(n > self.max_len for n in lengths):
             raise ValueError("a sequence is longer than max_len")
+        need = [max(0, -(-n // self.page_len) - self.held[s]) for s, n in enumerate(lengths)]
         if sum(need) > len(self.free):
             raise MemoryError("%d pages are wanted and %d are free" % (sum(need), len(self.free)))
         if not any(need):
@@ -49,6 +53,8 @@ class PagedCaches:
 
     def release(self, place: int) -> None:
         """The pages of a place are free again; its line of the table names none."""
+        if not 0 <= place < len(self.held):
+            raise ValueError("place %d of %d" % (place, len(self.held)))
         self.free.extend(int(p) for p in self.host_table[place, :self.held[place]])
         self.host_table[place] = -1
         self.held[place] = 0

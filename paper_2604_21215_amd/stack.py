@@ -76,14 +76,23 @@ class DeviceStack:
         w = self.lm_head.view(torch.int16).cpu().numpy().view("uint16") if self.dtype == "bf16" else self.lm_head.cpu().numpy()
         self.head4 = tuple(torch.from_numpy(a).to(self.device) for a in binding.rt_mx4_pack(w))
 
+    def _check_caches(self, caches: PagedCaches, S: int):
+        if len(caches.layer) != len(self.layers) or S > len(caches.held):
+            raise ValueError("caches of %d layers and at least %d places are required" % (len(self.layers), S))
+
     def into_pages(self, caches: PagedCaches, lens):
-        """The pairs that the last prefill left in self.K, self.V, rows 0 .. lens[b] - 1 of sequence b, into the pages of place b (which are
-        reserved here, with room for the next token).  lens[b] < 0: nothing of sequence b."""
-        caches.reserve([int(n) + 1 if n >= 0 else 0 for n in lens])
-        count = torch.tensor([max(int(n), 0) for n in lens], dtype=torch.int32, device=self.device)
+        """The pairs that the last prefill (and the decode_steps behind it) left in self.K, self.V, rows 0 .. lens[b] - 1 of sequence b, into
+        the pages of place b (which are reserved here, with room for the next token).  One length for each sequence of the prefill;
+        lens[b] < 0: nothing of sequence b."""
+        lens = [int(n) for n in lens]
+        if self.K is None or len(lens) != self.K[0].shape[1] or max(lens) > self.K[0].shape[0]:
+            raise ValueError("one length, of at most kv_cap, for each sequence of a prefill")
+        self._check_caches(caches, len(lens))
+        caches.reserve([n + 1 if n >= 0 else 0 for n in lens])
+        count = torch.tensor([max(n, 0) for n in lens], dtype=torch.int32, device=self.device)
         first = torch.tensor([0 if n >= 0 else -1 for n in lens], dtype=torch.int32, device=self.device)
+        N = max(max(lens), 1)
         for l in range(len(self.layers)):
-            N = max(max(int(n) for n in lens), 1)
             self.ctx.rt_cache_write(caches.layer[l], first, count, self.K[l][:N].transpose(0, 1), self.V[l][:N].transpose(0, 1))
 
     def decode_step_paged(self, caches: PagedCaches, ids: torch.Tensor, pos: torch.Tensor, max_pos: int, head4: bool = False):
@@ -91,6 +100,12 @@ class DeviceStack:
         max_pos; negative: an idle place, whose rows hold nothing).  The pages have been reserved for pos[s] + 1 positions.  Returns (logits
         [S, vocab] fp32, per-layer outputs [L, S, d]); head4: the read-out with the 4-bit weights of pack_lm_head."""
         S, L = ids.shape[0], len(self.layers)
+        for t in (ids, pos):   # the kernels follow their addresses
+            if t.dtype != torch.int32 or t.shape != (S,) or not t.is_contiguous() or t.device != self.embedding.device:
+                raise ValueError("ids and pos are contiguous int32 [S] on the stack's device")
+        if head4 and self.head4 is None:
+            raise ValueError("pack_lm_head comes first")
+        self._check_caches(caches, S)
         rows = torch.zeros((L + 1, S, 1, self.d), dtype=torch_dtype(self.dtype), device=self.device)
         self.ctx.rt_embed_rows(self.embedding, ids.view(S, 1), 0, rows[0])
         for l, lay in enumerate(self.layers):
