@@ -60,7 +60,8 @@ RT_BOTH uint32_t exponent_inverse_bits(int byte) { return byte == 0 || byte == 2
 //   wavefronts, one part.  Up to 256 positions four have enough to do.
 //   Else few pairs are cut until the chip has something to do (kWantGroups workgroups, parts of kShort positions and more), and all of them into
 //   parts of about kLong, which bounds how long one sequence of a ragged batch keeps its workgroup after the others are done.
-//   Many pairs, long rows in the storage dtype: sixteen wavefronts again, which end their sequences four times as early.
+//   Many pairs, long rows in the storage dtype (kMany16 positions, between the 2000 and the 4000 measured below): sixteen
+//   wavefronts again, which end their sequences four times as early.
 // MI355X, us per call, S H pairs of up to so many positions, waves * parts (bf16 unless said):
 //   16 pairs, 500: 4*1 6.0, 16*1 5.6;  1000: 4*1 8.7, 4*4 7.7, 16*1 7.3;  2000: 4*1 14.3, 4*8 7.8, 16*1 10.5;  14 pairs, 513, fp32: 4*1 7.7, 16*1 5.8;
 //   64 pairs, 1000: 4*4 8.0, 16*1 7.3;  2000: 4*8 8.6, 16*1 10.6;  8000: 4*1 62, 4*16 17.6, 16*4 17.0;
@@ -73,13 +74,13 @@ struct SplitPlan {
 };
 constexpr int kMaxPartials = 65536;    // stored partial states of a call: S * H * n_splits if n_splits > 1
 constexpr int kSplitUnit = 256;        // four wavefronts of 64 positions
-constexpr int kFewPairs = 256, kWhole16 = 1280, kLong16 = 4096;
+constexpr int kFewPairs = 256, kWhole16 = 1280, kLong16 = 4096, kMany16 = 3200;
 constexpr int kWantGroups = 768, kShort = 256, kWhole = 640, kLong = 1024;
 RT_BOTH SplitPlan split_plan(int max_len, int S, int H, bool eight_bits)
 {
     const int64_t pairs = (int64_t)S * H;
     const bool few = pairs <= kFewPairs && max_len > 256 && max_len <= (2 * pairs > kFewPairs ? kLong16 : kWhole16);
-    const bool many = pairs > kFewPairs && !eight_bits && max_len >= kLong16 * 3 / 4;
+    const bool many = pairs > kFewPairs && !eight_bits && max_len >= kMany16;
     int64_t n = kWantGroups / pairs;
     const int64_t most = max_len <= kWhole ? 1 : (max_len + kShort - 1) / kShort;
     if (n > most) n = most;
