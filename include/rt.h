@@ -342,7 +342,7 @@ rt_status rt_paged_attention(rt_ctx *ctx, const rt_paged_cache *cache, int32_t S
  *   plain ALUs, eight rows a launch).  q and the temporary pair stay in fp32; bf16 products take each vector as head and remainder.
  *   A few sequences of one length are better served by rt_decode_step's single launch over a contiguous cache (d = 1024, 512 positions, 8
  *   sequences: 26 us against 38); from 64 sequences on this call is the faster one (75 against 68, 8 bits 62; 200: 151 against 144, 8 bits 100).
- *   Scratch, capture: as rt_paged_attention. */
+ *   Equal calls give equal bits.  Scratch, capture: as rt_paged_attention. */
 rt_status rt_decode_step_paged(rt_ctx *ctx, const rt_layer_weights *w, const rt_paged_cache *cache, const void *x_t, int32_t S,
                                const int32_t *pos, int32_t max_pos, void *y_t);
 

@@ -29,6 +29,7 @@
 #include "rt_base_case.h"
 #include "rt_cross_tile.h"
 #include "rt_prepass_device.h"
+#include "rt_ll.h"
 
 namespace rt {
 
@@ -417,18 +418,27 @@ __device__ __forceinline__ void mm_body(const WaveLayer &Y, int t, int block_x, 
                                       cb, g, d / 16, d, eps);
     if (XL && EPI == EPI_QKV) {
         // a decoding step's input rows x_t [B][d] (Y.x, rows d apart) become the operand rows right here: head + remainder of
-        // x * g_attn, and the 1/rms of x from sums that meet in LDS (no separate preparation launch)
-        if (tid < 16) hss[tid] = 0.f;
+        // x * g_attn, and the 1/rms of x from sums that meet in LDS (no separate preparation launch).  K is a multiple of 256: the 64
+        // pieces of a wavefront belong to one row.  Each wavefront adds up its own pieces of a row, and the wavefronts' sums are added
+        // in their order: equal calls give equal bits, which sums in the order of arrival do not.
+        static_assert(EPI != EPI_QKV || 16 * NW <= 64, "hss holds one sum of each row for each wavefront");
+        if (tid < 16 * NW) hss[tid] = 0.f;
         __syncthreads();
         const bf16_t *xin = (const bf16_t *)Y.x;
         const bf16_t *ga = (const bf16_t *)Y.W.g_attn;
         const int ppr = K / 4;   // 4-element pieces per row
+        float sq = 0.f;
         for (int p = tid; p < Bn * ppr; p += 64 * NW) {
             const int r = p / ppr, e0 = (p - r * ppr) * 4;
             const uint2 xr = *reinterpret_cast<const uint2 *>(xin + (size_t)(b0 + r) * d + e0);
             float v[4] = {__uint_as_float(xr.x << 16), __uint_as_float(xr.x & 0xFFFF0000u), __uint_as_float(xr.y << 16),
                           __uint_as_float(xr.y & 0xFFFF0000u)};
-            atomicAdd(&hss[r], (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]));
+            sq += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]);
+            if (p + 64 * NW >= (r + 1) * ppr) {   // this wavefront's last pieces of the row, the same for all lanes
+                sq = fast_sum(sq);
+                if (lane == 0) hss[wave * 16 + r] = sq;
+                sq = 0.f;
+            }
             if (ga && !norm_free) {
                 const uint2 gr = *reinterpret_cast<const uint2 *>(ga + e0);
                 v[0] *= __uint_as_float(gr.x << 16); v[1] *= __uint_as_float(gr.x & 0xFFFF0000u);
@@ -437,7 +447,12 @@ __device__ __forceinline__ void mm_body(const WaveLayer &Y, int t, int block_x, 
             split_store4(xs, (size_t)(2 * r) * xld + e0, (size_t)(2 * r + 1) * xld + e0, v);
         }
         __syncthreads();
-        if (do_norm) rscale = rsqrtf(hss[cb] / (float)d + eps);
+        if (do_norm) {
+            float tot = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) tot += hss[w * 16 + cb];
+            rscale = rsqrtf(tot / (float)d + eps);
+        }
     } else if (XL) {
         const int ppr = K / 8;   // 16-byte pieces per operand row
         for (int p = tid; p < 2 * Bn * ppr; p += 64 * NW) {
