@@ -287,8 +287,9 @@ rt_status rt_lm_head(rt_ctx *ctx, const void *W_lm, const void *g_final, int32_t
  * numbers in table, first, count, lens and pos are read on the device: they may change between replays of a captured call, while
  * the sizes passed by value bound them.  None of these calls is limited by max_seq (a context for them alone needs max_seq = 1).
  *   8 bits: a row of 64 values u (one position, one head) is held as codes c = round(u / 2^e), ties to even, |c| <= 127, with the
- *   smallest e >= -126 for which every value fits, and the byte e + 127; it reads as c 2^e, off by at most 2^e / 2 <= max |u| / 127,
- *   exactly representable in bf16.  Byte 0: a row of zeros.  Byte 255: a value was not finite; the row reads as NaN.
+ *   smallest e >= -126 for which every value fits, and the byte e + 127; it reads as c 2^e, off by at most 2^e / 2 <=
+ *   max(max |u| / 127, 2^-127), exactly representable in bf16.  Values beyond 63.5 2^122 (3.376e38), whose codes at e = 122 would read as
+ *   infinities, are held as 63 2^122.  Byte 0: a row of zeros.  Byte 255: a value was not finite; the row reads as NaN.
  *   A table entry outside [0, pages) names no page: it is never followed.  Rows written there are dropped, rows read from there are
  *   NaN, an attention over it gives a row of NaN.  Entries past a sequence's last position are not looked at. */
 typedef struct {

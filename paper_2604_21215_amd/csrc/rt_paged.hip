@@ -115,13 +115,15 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const PagedCache C, co
 #pragma unroll
         for (int e = 0; e < PL; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
         const int byte = row_exponent(row_max_bits<LPR>(top));
-        const float inv = __uint_as_float(exponent_inverse_bits(byte));
+        if (__builtin_expect(byte == kLargestStep, 0)) {   // a branch of its own: as part of every code it costs 5 % of a large call
+#pragma unroll
+            for (int e = 0; e < PL; ++e) f[e] = row_clip(f[e]);
+        }
         uint32_t packed[PL / 4];
 #pragma unroll
         for (int e = 0; e < PL; ++e) {
-            const int code = byte == 255 ? 0 : (int)rintf(f[e] * inv);
             if (e % 4 == 0) packed[e / 4] = 0;
-            packed[e / 4] |= (uint32_t)(code & 255) << (8 * (e % 4));
+            packed[e / 4] |= (uint32_t)(row_code(f[e], byte) & 255) << (8 * (e % 4));
         }
         uint32_t *dst = reinterpret_cast<uint32_t *>((int8_t *)(w ? C.V : C.K) + row * kHeadDim + c * PL);
 #pragma unroll
@@ -542,8 +544,7 @@ __global__ __launch_bounds__(64) void paged_finish_kernel(const PagedCache C, co
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
         const int byte = row_exponent(top);
-        const int code = byte == 255 ? 0 : (int)rintf(u * __uint_as_float(exponent_inverse_bits(byte)));
-        ((int8_t *)(w ? C.V : C.K))[row * kHeadDim + lane] = (int8_t)code;
+        ((int8_t *)(w ? C.V : C.K))[row * kHeadDim + lane] = (int8_t)row_code(byte == kLargestStep ? row_clip(u) : u, byte);
         if (lane == 0) (w ? C.Vx : C.Kx)[row] = (uint8_t)byte;
     }
 }

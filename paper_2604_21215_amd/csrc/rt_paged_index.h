@@ -1,6 +1,7 @@
 // Arithmetic of the paged cache that is the same on the host and on the device (plain C++, no HIP types): where a row lies,
 // which exponent an 8-bit row takes, and how a call's positions are cut into splits.
 #pragma once
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -39,7 +40,7 @@ RT_BOTH bool page_ok(int entry, int pages) { return (uint32_t)entry < (uint32_t)
 // 8-bit rows: the values u of a row are held as codes rint(u 2^-e), |code| <= 127, with the smallest e >= -126 for which
 // max |u| <= 127 2^e, and the byte e + 127.  Steps are powers of two: u 2^-e and code 2^e are exact, so a code never depends on how a
 // quotient was rounded, and what is read back is exact in bf16 as well (seven bits).  Byte 0: all values are 0.  Byte 255: a value of
-// the row is not finite; the row reads as NaN.
+// the row is not finite; the row reads as NaN.  At the largest step, 2^122 (byte 249), the code 64 would read as 2^128: codes end at 63 there.
 // top: the largest of the row's values as bits, sign cleared (as integers these order like the values, NaN above all).
 RT_BOTH int row_exponent(uint32_t top)
 {
@@ -52,6 +53,15 @@ RT_BOTH int row_exponent(uint32_t top)
 }
 RT_BOTH uint32_t exponent_step_bits(int byte) { return byte == 255 ? 0x7FC00000u : (uint32_t)byte << 23; }          // 2^e, 0 or NaN
 RT_BOTH uint32_t exponent_inverse_bits(int byte) { return byte == 0 || byte == 255 ? 0u : (uint32_t)(254 - byte) << 23; }   // 2^-e, or 0
+constexpr int kLargestStep = 249;
+RT_BOTH float row_clip(float u) { return fminf(fmaxf(u, -0x1.f8p127f), 0x1.f8p127f); }   // to 63 steps of the largest
+RT_BOTH int row_code(float u, int byte)   // the code of a value (clipped, if the byte is kLargestStep) of a row with this byte
+{
+    const uint32_t inv_bits = exponent_inverse_bits(byte);
+    float inv;
+    __builtin_memcpy(&inv, &inv_bits, 4);
+    return byte == 255 ? 0 : (int)rintf(u * inv);
+}
 
 // How the positions below max_len of S sequences and H heads are cut: workgroups of `waves` wavefronts and split_len positions each (the last
 // one shorter).  A cut costs a second launch and a stored state per part; a workgroup of sixteen wavefronts has as many loads on the way as four

@@ -206,10 +206,9 @@ __device__ __forceinline__ void page_store(const StepPages &out, const float *v,
         return;
     }
     const int byte = row_exponent(top);
-    const float inv = __uint_as_float(exponent_inverse_bits(byte));
     uint32_t packed = 0;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) packed |= (uint32_t)((byte == 255 ? 0 : (int)rintf(v[r] * inv)) & 255) << (8 * r);
+    for (int r = 0; r < 4; ++r) packed |= (uint32_t)(row_code(byte == kLargestStep ? row_clip(v[r]) : v[r], byte) & 255) << (8 * r);
     *reinterpret_cast<uint32_t *>((int8_t *)dst + at) = packed;
     if (rg == 0 && g == 0) (is_k ? C.Kx : C.Vx)[row] = (uint8_t)byte;
 }
