@@ -307,7 +307,8 @@ typedef struct {
  *   bytes, at least d_model): seq_stride = d_model, pos_stride = B d_model for the caches of rt_layer_prefill and rt_decode_step.
  *   count[s] is cut to [0, N]; count NULL = N for every sequence.  first[s] < 0: an idle place, nothing is written for it.  Positions
  *   past table_stride * page_len are dropped.  Two rows of one call that name the same place race.
- *   1 <= S <= 65535, 1 <= N <= 2^20, N n_heads <= 2^30.  No scratch is used; S is not limited by max_batch. */
+ *   1 <= S <= 65535, 1 <= N <= 2^20, N (rounded up to a multiple of 8) n_heads <= 2^29 - 32 (bf16) or 2^28 - 16 (fp32).  No scratch is used;
+ *   S is not limited by max_batch. */
 rt_status rt_cache_write(rt_ctx *ctx, const rt_paged_cache *cache, int32_t S, const int32_t *first, const int32_t *count, int32_t N,
                          const void *k, const void *v, int64_t seq_stride, int64_t pos_stride);
 

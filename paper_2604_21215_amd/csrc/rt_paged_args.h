@@ -63,8 +63,8 @@ inline rt_status check_pair_rows(const rt_config &cfg, const PoolRanges &pool, c
     const int64_t d = cfg.d_model, E = storage_bytes(cfg), most = (int64_t)1 << 40;
     *msg = "null pointer";
     if (!first || !k || !v) return RT_ERR_INVALID_ARG;
-    *msg = "1 <= N <= 2^20 and N n_heads <= 2^30 are required";
-    if (N < 1 || N > (1 << 20) || (int64_t)N * cfg.n_heads > (1 << 30)) return RT_ERR_INVALID_ARG;
+    *msg = "1 <= N <= 2^20 and N (rounded up to a multiple of 8) n_heads <= 2^29 - 32 (bf16) or 2^28 - 16 (fp32) are required";
+    if (N < 1 || N > (1 << 20) || pair_row_lanes(N, cfg.n_heads, E) > kMaxRowLanes) return RT_ERR_INVALID_ARG;
     *msg = "rows are at least d_model elements apart";
     if ((S > 1 && seq_stride < d) || (N > 1 && pos_stride < d) || seq_stride < 0 || pos_stride < 0 || seq_stride > most || pos_stride > most)
         return RT_ERR_INVALID_ARG;

@@ -34,6 +34,11 @@ struct StepPages {
     int max_pos;
 };
 
+// Work-items in x of the launch over N rows of S sequences: a lane for every 16 bytes of a row, positions in tiles of eight.  A grid has
+// fewer than 2^32 of them.
+RT_BOTH int64_t pair_row_lanes(int64_t N, int64_t H, int64_t storage_bytes) { return (N + 7) / 8 * 8 * H * (64 * storage_bytes / 16); }
+constexpr int64_t kMaxRowLanes = ((int64_t)1 << 32) - 256;   // whole workgroups of 256
+
 // A page table's entry is used only if it names a page of the pool.
 RT_BOTH bool page_ok(int entry, int pages) { return (uint32_t)entry < (uint32_t)pages; }
 

@@ -42,9 +42,35 @@ static int codes()
     return 0;
 }
 
+// What the checks accept can be launched: fewer than 2^32 work-items in x, in whole workgroups (rows_grid: a workgroup of 256 takes 32 rows in
+// bf16 and 16 in fp32, positions in tiles of eight from N = 8 on).
+static int launches()
+{
+    const char *msg;
+    const int32_t *ints = (const int32_t *)(uintptr_t)(1ull << 40);
+    for (int dtype : {RT_BF16, RT_F32})
+        for (int H : {1, 255, 256, 257, 511, 512, 513, 1000, 18631, 4096, 100000}) {
+            rt_config c = {};
+            c.n_heads = H; c.head_dim = 64; c.d_model = 64 * H; c.max_batch = 1; c.dtype = dtype;
+            const int per = dtype == RT_BF16 ? 32 : 16;
+            const int64_t limit = dtype == RT_BF16 ? 1ll << 29 : 1ll << 28;
+            const int mid = (int)(limit / H);
+            for (int N : {1, 7, 8, 9, 14408, mid - 9, mid - 8, mid - 7, mid - 1, mid, mid + 1, mid + 9, (1 << 20) - 7, 1 << 20, (1 << 20) + 1}) {
+                if (N < 1) continue;
+                const int64_t d = c.d_model;
+                const bool ok = check_pair_rows(c, PoolRanges{}, ints, 1, N, (const void *)(2ull << 50), (const void *)(3ull << 50), d, d, false, &msg) == RT_OK;
+                const int64_t rows = N >= 8 ? (int64_t)((N + 7) / 8) * 8 * H : (int64_t)N * H, items = (rows + per - 1) / per * 256;
+                if (ok) EXPECT(items < 1ll << 32 && N <= 1 << 20);
+                EXPECT(ok == (N <= 1 << 20 && (int64_t)(N + 7) / 8 * 8 * H <= limit - per));
+            }
+        }
+    return 0;
+}
+
 int main(int argc, char **argv)
 {
     const char *what = argc > 1 ? argv[1] : "";
     if (!strcmp(what, "codes")) return codes();
+    if (!strcmp(what, "launches")) return launches();
     return 2;
 }
