@@ -323,7 +323,7 @@ rt_status rt_cache_read(rt_ctx *ctx, const rt_paged_cache *cache, int32_t S, con
  *   out: rows out_stride elements apart, written in the storage dtype; lse [S][n_heads] fp32 or NULL: log sum exp of the row's logits.
  *   lens[s] < 0: an idle place of a padded batch, its rows of out and lse are left as they were.  No cached row and no pair, or no logit
  *   above minus infinity: out 0, lse minus infinity.  lens[s] > max_len: NaN.
- *   1 <= S <= max_batch, 0 <= max_len <= min(2^20, table_stride * page_len); the work is laid out for max_len.
+ *   1 <= S <= max_batch, 0 <= max_len <= min(2^20, table_stride * page_len); the work is laid out for max_len.  out and lse overlap nothing else.
  *   fp32 sums and softmax.  Results do not depend on other sequences of the call but for max_len and S, by which the cache is cut into
  *   parts whose softmax states are joined in their order: equal calls give equal bits.
  *   The first call allocates scratch (18 MB, kept until rt_destroy) unless RT_RESERVE_PAGED reserved it at rt_create; a call on a stream that
@@ -358,7 +358,7 @@ rt_status rt_mx4_pack(const void *W, int32_t dtype, int64_t rows, int32_t cols, 
 /* rt_lm_head with such a matrix: logits[b, v] = < W4[v, :], RMS(z_b; g_final) >, fp32 accuracy for the weights as they are packed.
  *   codes [vocab][d / 2] (on 16 bytes), exps [vocab][d / 32] device; a scale byte of 0 or 255 makes its row's logits NaN,
  *   a weight past fp32's range makes them infinite or NaN.  Other arguments
- *   as rt_lm_head; d_model <= 25856; logits must not overlap an input. */
+ *   as rt_lm_head; d_model <= 25856, vocab < 2^31 - 64; logits must not overlap an input. */
 rt_status rt_lm_head_mx4(rt_ctx *ctx, const uint8_t *codes, const uint8_t *exps, const void *g_final, int32_t vocab, const void *z,
                          int64_t z_stride, int32_t B, float *logits);
 

@@ -1328,7 +1328,8 @@ extern "C" rt_status rt_cache_write(rt_ctx *c, const rt_paged_cache *cache, int3
     PoolRanges pool;
     const char *msg;
     rt_status s = check_pool(c->cfg, cache, S, &pool, &msg);
-    if (s == RT_OK) s = check_pair_rows(c->cfg, pool, first, S, N, k, v, seq_stride, pos_stride, false, &msg);
+    if (s == RT_OK) s = check_pair_rows(c->cfg, pool, first, S, N, k, v, seq_stride, pos_stride, false, &msg, count, cache->table,
+                                        cache->table_stride);
     if (s != RT_OK) return fail(c, s, "%s", msg);
     if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(c, RT_ERR_HIP, "hipSetDevice failed%s");
     const PagedCache C = to_pool(*cache);
@@ -1347,7 +1348,8 @@ extern "C" rt_status rt_cache_read(rt_ctx *c, const rt_paged_cache *cache, int32
     PoolRanges pool;
     const char *msg;
     rt_status s = check_pool(c->cfg, cache, S, &pool, &msg);
-    if (s == RT_OK) s = check_pair_rows(c->cfg, pool, first, S, N, k, v, seq_stride, pos_stride, true, &msg);
+    if (s == RT_OK) s = check_pair_rows(c->cfg, pool, first, S, N, k, v, seq_stride, pos_stride, true, &msg, count, cache->table,
+                                        cache->table_stride);
     if (s != RT_OK) return fail(c, s, "%s", msg);
     if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(c, RT_ERR_HIP, "hipSetDevice failed%s");
     const PagedCache C = to_pool(*cache);
@@ -1462,7 +1464,7 @@ extern "C" rt_status rt_lm_head_mx4(rt_ctx *c, const uint8_t *codes, const uint8
     if (!c) return RT_ERR_INVALID_ARG;
     if (c->broken) return fail(c, RT_ERR_STATE, "context is unusable after an earlier failure%s");
     const char *msg;
-    const rt_status s = check_mx4_head(c->cfg, codes, exps, vocab, z, z_stride, B, logits, &msg);
+    const rt_status s = check_mx4_head(c->cfg, codes, exps, vocab, z, z_stride, B, logits, &msg, g_final);
     if (s != RT_OK) return fail(c, s, "%s", msg);
     if (hipSetDevice(c->cfg.device) != hipSuccess) return fail(c, RT_ERR_HIP, "hipSetDevice failed%s");
     const int nf = (c->cfg.flags & RT_FLAG_NORM_FREE) ? 1 : 0;

@@ -30,6 +30,13 @@ struct PoolRanges {
     bool meets(const ByteRange &o) const { return ranges_meet(r[0], o) || ranges_meet(r[1], o) || ranges_meet(r[2], o) || ranges_meet(r[3], o); }
 };
 
+// The lines of S sequences in a table of which the last line's first `entries` count.
+inline ByteRange table_range(const rt_paged_cache &cache, int32_t S, int64_t entries)
+{
+    return {cache.table, (size_t)(((int64_t)(S - 1) * cache.table_stride + (entries < 1 ? 1 : entries)) * 4)};
+}
+inline ByteRange ints_range(const int32_t *p, int32_t S) { return {p, (size_t)S * 4}; }
+
 inline rt_status check_pool(const rt_config &cfg, const rt_paged_cache *cache, int32_t S, PoolRanges *out, const char **msg)
 {
     *msg = "null cache pointer";
@@ -52,13 +59,16 @@ inline rt_status check_pool(const rt_config &cfg, const rt_paged_cache *cache, i
     for (int i = 0; i < 4; ++i)
         for (int j = 0; j < i; ++j)
             if (ranges_meet(out->r[i], out->r[j])) return RT_ERR_INVALID_ARG;
+    *msg = "the page table must not overlap the pages";
+    if (out->meets(table_range(*cache, S, 1))) return RT_ERR_INVALID_ARG;
     *msg = "";
     return RT_OK;
 }
 
 // Rows of pairs on the caller's side; outputs: rows that are written must not overlap one another.
 inline rt_status check_pair_rows(const rt_config &cfg, const PoolRanges &pool, const int32_t *first, int32_t S, int32_t N, const void *k,
-                                 const void *v, int64_t seq_stride, int64_t pos_stride, bool outputs, const char **msg)
+                                 const void *v, int64_t seq_stride, int64_t pos_stride, bool outputs, const char **msg,
+                                 const int32_t *count = nullptr, const int32_t *table = nullptr, int64_t table_stride = 0)
 {
     const int64_t d = cfg.d_model, E = storage_bytes(cfg), most = (int64_t)1 << 40;
     *msg = "null pointer";
@@ -74,6 +84,10 @@ inline rt_status check_pair_rows(const rt_config &cfg, const PoolRanges &pool, c
     const ByteRange kr = {k, span}, vr = {v, span};
     *msg = "the rows must not overlap the cache";
     if (pool.meets(kr) || pool.meets(vr)) return RT_ERR_INVALID_ARG;
+    const ByteRange ints[3] = {ints_range(first, S), ints_range(count, S), {table, (size_t)((S - 1) * table_stride + 1) * 4}};
+    *msg = "first, count and the page table must not overlap what is written";
+    for (const ByteRange &r : ints)
+        if (outputs ? ranges_meet(kr, r) || ranges_meet(vr, r) : pool.meets(r)) return RT_ERR_INVALID_ARG;
     if (outputs) {
         *msg = "the rows of different sequences overlap";
         if (S > 1 && N > 1 && seq_stride < (int64_t)(N - 1) * pos_stride + d && pos_stride < (int64_t)(S - 1) * seq_stride + d)
@@ -117,6 +131,8 @@ inline rt_status check_paged_attention(const rt_config &cfg, const rt_paged_cach
     if (ranges_meet(o, l) || pool.meets(o) || pool.meets(l)) return RT_ERR_INVALID_ARG;
     for (const ByteRange &r : in)
         if (ranges_meet(o, r) || ranges_meet(l, r)) return RT_ERR_INVALID_ARG;
+    const ByteRange n = ints_range(lens, S), t = table_range(*cache, S, (max_len + cache->page_len - 1) / cache->page_len);
+    if (ranges_meet(o, n) || ranges_meet(l, n) || ranges_meet(o, t) || ranges_meet(l, t)) return RT_ERR_INVALID_ARG;
     *msg = "";
     return RT_OK;
 }
@@ -136,18 +152,21 @@ inline rt_status check_paged_step(const rt_config &cfg, const rt_paged_cache *ca
     const ByteRange x = {x_t, bytes}, y = {y_t, bytes};
     *msg = "the cache, x_t, y_t must not overlap";
     if (ranges_meet(x, y) || pool.meets(x) || pool.meets(y)) return RT_ERR_INVALID_ARG;
+    const ByteRange n = ints_range(pos, S);
+    *msg = "pos and the page table must not overlap y_t or the cache";
+    if (ranges_meet(y, n) || pool.meets(n) || ranges_meet(y, table_range(*cache, S, max_pos / cache->page_len + 1))) return RT_ERR_INVALID_ARG;
     *msg = "";
     return RT_OK;
 }
 
 inline rt_status check_mx4_head(const rt_config &cfg, const uint8_t *codes, const uint8_t *exps, int32_t vocab, const void *z, int64_t z_stride,
-                                int32_t B, const float *logits, const char **msg)
+                                int32_t B, const float *logits, const char **msg, const void *g_final = nullptr)
 {
     const int64_t d = cfg.d_model;
     *msg = "null pointer";
     if (!codes || !exps || !z || !logits) return RT_ERR_INVALID_ARG;
-    *msg = "vocab >= 1, 1 <= B <= max_batch and z_stride >= d_model are required";
-    if (vocab < 1 || B < 1 || B > cfg.max_batch || z_stride < d || z_stride > (int64_t)1 << 40) return RT_ERR_INVALID_ARG;
+    *msg = "1 <= vocab < 2^31 - 64, 1 <= B <= max_batch and z_stride >= d_model are required";
+    if (vocab < 1 || vocab >= INT32_MAX - 63 || B < 1 || B > cfg.max_batch || z_stride < d || z_stride > (int64_t)1 << 40) return RT_ERR_INVALID_ARG;
     *msg = "the codes must lie on 16 bytes";
     if (!on16(codes)) return RT_ERR_INVALID_ARG;
     *msg = "rt_lm_head_mx4 covers d_model <= 25856";
@@ -155,7 +174,8 @@ inline rt_status check_mx4_head(const rt_config &cfg, const uint8_t *codes, cons
     const ByteRange l = {logits, (size_t)B * (size_t)vocab * 4};
     *msg = "logits must not overlap an input";
     if (ranges_meet(l, {z, (size_t)(((B - 1) * z_stride + d) * storage_bytes(cfg))}) ||
-        ranges_meet(l, {codes, (size_t)vocab * (size_t)d / 2}) || ranges_meet(l, {exps, (size_t)vocab * (size_t)d / kMx4Block}))
+        ranges_meet(l, {codes, (size_t)vocab * (size_t)d / 2}) || ranges_meet(l, {exps, (size_t)vocab * (size_t)d / kMx4Block}) ||
+        ranges_meet(l, {g_final, (size_t)(d * storage_bytes(cfg))}))
         return RT_ERR_INVALID_ARG;
     *msg = "";
     return RT_OK;

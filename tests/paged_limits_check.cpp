@@ -67,10 +67,66 @@ static int launches()
     return 0;
 }
 
+static char *at(uint64_t v) { return (char *)(uintptr_t)v; }   // addresses are compared, never followed
+
+// What a call writes must not be what it reads while it writes: lengths, positions, the page table, the gain of the read-out.
+static int overlaps()
+{
+    const char *msg;
+    PoolRanges R;
+    rt_config c = {};
+    c.d_model = 256; c.n_heads = 4; c.head_dim = 64; c.max_batch = 8; c.dtype = RT_BF16;
+    rt_paged_cache p = {};
+    p.K = at(1ull << 40); p.V = at(2ull << 40); p.table = (const int32_t *)at(5ull << 40);
+    p.table_stride = 10; p.pages = 20; p.page_len = 32;
+    EXPECT(check_pool(c, &p, 3, &R, &msg) == RT_OK);
+    rt_paged_cache inside = p;
+    inside.table = (const int32_t *)at((1ull << 40) + 64);
+    EXPECT(check_pool(c, &inside, 3, &R, &msg) == RT_ERR_INVALID_ARG);
+    inside.table = (const int32_t *)at((2ull << 40) - 84);      // the third line's first entry is the pool's first byte
+    EXPECT(check_pool(c, &inside, 3, &R, &msg) == RT_OK);
+    inside.table = (const int32_t *)at((2ull << 40) - 80);
+    EXPECT(check_pool(c, &inside, 3, &R, &msg) == RT_ERR_INVALID_ARG && check_pool(c, &inside, 2, &R, &msg) == RT_OK);
+    EXPECT(check_pool(c, &p, 3, &R, &msg) == RT_OK);
+
+    char *k = at(7ull << 40), *v = at(8ull << 40), *q = at(9ull << 40), *out = at(10ull << 40);
+    const int32_t *ints = (const int32_t *)at(6ull << 40);
+    auto rows = [&](const int32_t *first, const int32_t *count, const int32_t *table, bool outputs) {
+        return check_pair_rows(c, R, first, 3, 5, k, v, 256, 768, outputs, &msg, count, table, 10);
+    };
+    for (bool outputs : {false, true}) {
+        EXPECT(rows(ints, nullptr, p.table, outputs) == RT_OK && rows(ints, ints, p.table, outputs) == RT_OK);
+        for (char *w : {k, v, (char *)p.K + 100, (char *)p.V}) {
+            const bool written = outputs == (w == k || w == v);
+            const int32_t *i = (const int32_t *)(w + 512);
+            EXPECT((rows(i, nullptr, p.table, outputs) == RT_OK) == !written && (rows(ints, i, p.table, outputs) == RT_OK) == !written);
+            EXPECT((rows(ints, nullptr, i, outputs) == RT_OK) == !written);
+        }
+    }
+    float *lse = (float *)at(11ull << 40);
+    auto attn = [&](const int32_t *lens, void *o, float *l) {
+        return check_paged_attention(c, &p, R, 3, lens, 100, q, 256, k, v, 256, o, 256, l, &msg);
+    };
+    EXPECT(attn(ints, out, lse) == RT_OK && attn(ints, out, nullptr) == RT_OK);
+    EXPECT(attn((const int32_t *)(out + 4), out, lse) == RT_ERR_INVALID_ARG && attn((const int32_t *)(lse + 11), out, lse) == RT_ERR_INVALID_ARG);
+    EXPECT(attn(ints, (void *)(p.table + 23), lse) == RT_ERR_INVALID_ARG && attn(ints, (void *)(p.table + 24), lse) == RT_OK);   // 4 entries of the last line
+    EXPECT(attn(ints, out, (float *)p.table) == RT_ERR_INVALID_ARG);
+    auto step = [&](const int32_t *pos, void *y) { return check_paged_step(c, &p, R, q, 3, pos, 100, y, &msg); };
+    EXPECT(step(ints, out) == RT_OK && step((const int32_t *)out + 2, out) == RT_ERR_INVALID_ARG);
+    EXPECT(step((const int32_t *)p.K, out) == RT_ERR_INVALID_ARG && step(ints, (void *)p.table) == RT_ERR_INVALID_ARG);
+    const uint8_t *codes = (const uint8_t *)at(12ull << 40), *exps = (const uint8_t *)at(13ull << 40);
+    auto head = [&](int vocab, const void *g) { return check_mx4_head(c, codes, exps, vocab, q, 256, 8, lse, &msg, g); };
+    EXPECT(head(100, k) == RT_OK && head(100, nullptr) == RT_OK && head(100, lse + 799) == RT_ERR_INVALID_ARG && head(100, lse + 800) == RT_OK);
+    EXPECT(head(100, (char *)lse - 511) == RT_ERR_INVALID_ARG && head(100, (char *)lse - 512) == RT_OK);
+    EXPECT(head(INT32_MAX, k) == RT_ERR_INVALID_ARG && head(INT32_MAX - 63, k) == RT_ERR_INVALID_ARG && head(INT32_MAX - 64, k) == RT_OK);
+    return 0;
+}
+
 int main(int argc, char **argv)
 {
     const char *what = argc > 1 ? argv[1] : "";
     if (!strcmp(what, "codes")) return codes();
     if (!strcmp(what, "launches")) return launches();
+    if (!strcmp(what, "overlaps")) return overlaps();
     return 2;
 }

@@ -15,7 +15,7 @@ def program(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("check", ["codes", "launches"])
+@pytest.mark.parametrize("check", ["codes", "launches", "overlaps"])
 def test_paged_limits(program, check):
     r = subprocess.run([program, check], stdout=subprocess.PIPE, text=True, timeout=60)
     assert r.returncode == 0, r.stdout
