@@ -52,6 +52,8 @@ class rt_layer_grads(C.Structure):
 class rt_paged_cache(C.Structure):
     _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("K_exp", C.c_void_p), ("V_exp", C.c_void_p), ("table", C.c_void_p),
                 ("table_stride", C.c_int64), ("pages", C.c_int32), ("page_len", C.c_int32), ("bits", C.c_int32)]
+    # set by make_cache: heads, bytes of an element and device in one number (0: not known), and the table's lines
+    fit = 0, 1 << 31
 
 
 class RTError(RuntimeError):
@@ -189,33 +191,60 @@ def make_weights(w: dict) -> rt_layer_weights:
     return s
 
 
+_INTS = "lengths, positions and counts are contiguous int32, one for each sequence"
+
+
+def _invalid(msg):
+    raise RTError("RT_ERR_INVALID_ARG", msg)
+
+
+_dtypes = None
+
+
+def _load_dtypes():   # an import statement in a call costs as much as three of its checks
+    global _dtypes
+    import torch
+    _dtypes = torch.int8, torch.uint8, torch.int32
+    return _dtypes
+
+
+def _fit(heads, size, device):
+    return heads << 16 | size << 12 | device + 2
+
+
 def make_cache(K, V, table, K_exp=None, V_exp=None) -> rt_paged_cache:
     """K, V [pages, H, page_len, 64] (storage dtype, or int8 with the bytes K_exp, V_exp [pages, H, page_len]), table int32 [S, entries]."""
-    shape = K.shape
-    if not (K.is_contiguous() and V.is_contiguous()) or V.shape != shape or len(shape) != 4 or K.dtype != V.dtype:
-        raise RTError("RT_ERR_INVALID_ARG", "K, V are contiguous [pages, H, page_len, 64] of one type")
-    ke = ve = None
-    if K_exp is not None:
-        if V_exp is None or K_exp.shape != shape[:3] or V_exp.shape != shape[:3] or not (K_exp.is_contiguous() and V_exp.is_contiguous()):
-            raise RTError("RT_ERR_INVALID_ARG", "K_exp, V_exp are contiguous [pages, H, page_len]")
+    int8, uint8, int32 = _dtypes or _load_dtypes()
+    shape, dt, dev, ke, ve = K.shape, K.dtype, K.get_device(), None, None
+    pages, heads, page_len, width = shape if len(shape) == 4 else (0, 0, 0, 0)
+    if width != 64 or V.shape != shape or V.dtype is not dt or not (K.is_contiguous() and V.is_contiguous()):
+        _invalid("K, V are contiguous [pages, H, page_len, 64] of one type")
+    if dt is int8 or K_exp is not None or V_exp is not None:
+        if K_exp is None or V_exp is None or dt is not int8:
+            _invalid("K_exp, V_exp belong to a cache of 8 bits (K, V int8), and to no other")
+        for t in (K_exp, V_exp):
+            if t.dtype is not uint8 or t.shape != shape[:3] or not t.is_contiguous() or t.get_device() != dev:
+                _invalid("K_exp, V_exp are contiguous uint8 [pages, H, page_len] on the device of K")
         ke, ve = K_exp.data_ptr(), V_exp.data_ptr()
-    rows, entries = table.shape
-    if table.element_size() != 4 or (entries > 1 and table.stride(1) != 1):
-        raise RTError("RT_ERR_INVALID_ARG", "table is int32 [S, entries]")
-    return rt_paged_cache(K.data_ptr(), V.data_ptr(), ke, ve, table.data_ptr(), table.stride(0) if rows > 1 else entries, shape[0], shape[2],
-                          8 if K.element_size() == 1 else 0)
+    (lines, entries), (stride, inner) = table.shape, table.stride()
+    if table.dtype is not int32 or (inner != 1 and entries > 1):
+        _invalid("table is int32 [S, entries]")
+    if V.get_device() != dev or table.get_device() != dev:
+        _invalid("K, V and table lie on one device")
+    size = K.element_size()
+    c = rt_paged_cache(K.data_ptr(), V.data_ptr(), ke, ve, table.data_ptr(), stride if lines > 1 else entries, pages, page_len, 8 if size == 1 else 0)
+    c.fit = heads << 16 | size << 12 | dev + 2, lines
+    return c
 
 
-def _pair_strides(k, v):
-    """k, v [S, N, H, 64] with the same strides and the last two dimensions contiguous -> (seq_stride, pos_stride)."""
-    shape, stride = k.shape, k.stride()
-    if v.shape == shape and v.stride() == stride and stride[3] == 1 and stride[2] == shape[3]:
-        return stride[:2]
-    S, N, H, dh = shape   # dimensions of one row have no stride
-    strides = lambda t: (t.stride(0) if S > 1 else 0, t.stride(1) if N > 1 else 0, t.stride(2) if H > 1 else dh, t.stride(3))  # noqa: E731
-    if v.shape != shape or strides(v) != strides(k) or strides(k)[2:] != (dh, 1):
-        raise RTError("RT_ERR_INVALID_ARG", "k and v are [S, N, H, 64] with equal strides and contiguous heads")
-    return strides(k)[:2]
+def _pair_strides(k, v, H):
+    """k, v [S, N, H, 64] with the same strides and the last two dimensions contiguous, dimensions of one row apart, which have no stride."""
+    if len(k.shape) == 4 and v.shape == k.shape and tuple(k.shape[2:]) == (H, 64):
+        S, N = k.shape[:2]
+        strides = lambda t: (t.stride(0) if S > 1 else 0, t.stride(1) if N > 1 else 0, t.stride(2) if H > 1 else 64, t.stride(3))  # noqa: E731
+        if strides(v) == strides(k) and strides(k)[2:] == (64, 1):
+            return strides(k)[:2]
+    _invalid("k and v are [S, N, n_heads, 64] with equal strides and contiguous heads")
 
 
 def rt_mx4_pack(W):
@@ -351,56 +380,128 @@ class RTContext:
                                 _ptr(logits))
         _check(self._L, self._ctx, rc)
 
-    # The calls of a serving loop pass addresses as plain integers: a ctypes object per pointer costs as much as the call itself.
+    # The calls of a serving loop pass addresses as plain integers: a ctypes object per pointer costs as much as the call itself.  What the
+    # library cannot see behind an address is checked here: types, entries, inner strides.  The tests on the way of every call are written out
+    # in it, a function per tensor takes as long as the tests themselves.
+    _known = None
+
+    def _storage(self):
+        """What the checks compare with, read from the configuration once."""
+        import torch
+        cfg = self.cfg
+        H, size = cfg.n_heads, 2 if cfg.dtype == RT_BF16 else 4
+        self._known = (torch.bfloat16 if size == 2 else torch.float32, torch.int32, torch.float32, cfg.d_model, H, cfg.max_batch,
+                       (0, _fit(H, size, cfg.device), _fit(H, 1, cfg.device)))
+        return self._known
+
+    def _misfit(self, cache, S):
+        fit, lines = cache.fit
+        if fit not in self._known[6]:
+            _invalid("the cache has %d heads of %d-byte elements on device %d, the context %d of %d or 1 on %d" %
+                     (fit >> 16, fit >> 12 & 15, (fit & 4095) - 2, self.cfg.n_heads, 2 if self.cfg.dtype == RT_BF16 else 4, self.cfg.device))
+        _invalid("%d sequences and %d lines of the page table" % (S, lines))
+
+    def _rows(self, t, S):
+        """Elements between rows that are not simply one behind the other (a dimension of one row has no stride)."""
+        shape, stride, d = t.shape, t.stride(), self._known[3]
+        if t.dtype is self._known[0] and shape[0] >= S and (
+                (len(shape) == 2 and shape[1] == d and stride[1] == 1) or
+                (len(shape) == 3 and shape[1] * shape[2] == d and stride[2] == 1 and (stride[1] == shape[2] or shape[1] == 1))):
+            return stride[0] if S > 1 else d
+        _invalid("rows are [S, n_heads, 64] or [S, d_model] of the storage dtype, contiguous inside")
+
+    def _pairs(self, cache, first, count, k, v):
+        dt, i32, _, _, H, _, fits = self._known or self._storage()
+        shape, stride, cp = k.shape, k.stride(), None
+        if v.stride() == stride and stride[2:] == (64, 1) and v.shape == shape and shape[3] == 64 and shape[2] == H:
+            ss, ps, _, _ = stride
+        else:
+            ss, ps = _pair_strides(k, v, H)
+        S = shape[0]
+        if k.dtype is not dt or v.dtype is not dt:
+            _invalid("k and v are of the storage dtype")
+        fit, lines = cache.fit
+        if fit not in fits or S > lines:
+            self._misfit(cache, S)
+        if first.dtype is not i32 or first.numel() < S or not first.is_contiguous():
+            _invalid(_INTS)
+        if count is not None:
+            cp = count.data_ptr()
+            if count.dtype is not i32 or count.numel() < S or not count.is_contiguous():
+                _invalid(_INTS)
+        return self._ctx, cache, S, first.data_ptr(), cp, shape[1], k.data_ptr(), v.data_ptr(), ss, ps
 
     # -- rt_cache_write(ctx, cache, S, first[S] int32, count[S] int32 | None, N, k[S,N,H,64], v, seq_stride, pos_stride)
     def rt_cache_write(self, cache: rt_paged_cache, first, count, k, v):
-        S, N = k.shape[:2]
-        ss, ps = _pair_strides(k, v)
-        rc = self._L.rt_cache_write(self._ctx, cache, S, first.data_ptr(), None if count is None else count.data_ptr(), N, k.data_ptr(),
-                                    v.data_ptr(), ss, ps)
+        rc = self._L.rt_cache_write(*self._pairs(cache, first, count, k, v))
         if rc:
             _check(self._L, self._ctx, rc)
 
     # -- rt_cache_read(ctx, cache, S, first[S] int32, count[S] int32 | None, N, k[S,N,H,64], v, seq_stride, pos_stride)
     def rt_cache_read(self, cache: rt_paged_cache, first, count, k, v):
-        S, N = k.shape[:2]
-        ss, ps = _pair_strides(k, v)
-        rc = self._L.rt_cache_read(self._ctx, cache, S, first.data_ptr(), None if count is None else count.data_ptr(), N, k.data_ptr(),
-                                   v.data_ptr(), ss, ps)
+        rc = self._L.rt_cache_read(*self._pairs(cache, first, count, k, v))
         if rc:
             _check(self._L, self._ctx, rc)
 
     # -- rt_paged_attention(ctx, cache, S, lens[S] int32, max_len, q[S,H,64], q_stride, k_t | None, v_t | None, kv_stride, out, out_stride, lse[S,H] f32 | None)
     def rt_paged_attention(self, cache: rt_paged_cache, lens, max_len, q, k_t, v_t, out, lse=None):
-        """q, k_t, v_t, out [S, H, 64] (or [S, d]): rows at their first stride, contiguous inside."""
-        S, d = q.shape[0], self.cfg.d_model
-        qs, os_, ks, kp, vp = d, d, d, None, None
-        if S > 1:   # a dimension of one row has no stride
-            qs, os_ = q.stride(0), out.stride(0)
+        """q, k_t, v_t, out [S, H, 64] (or [S, d]): rows at their first stride, contiguous inside; lse [S, H]."""
+        dt, i32, f32, d, H, most, fits = self._known or self._storage()
+        S, kp, vp, lp, ks = q.shape[0], None, None, None, d
+        fit, lines = cache.fit
+        if (fit not in fits or S > lines) and S <= most:   # more than max_batch are refused by the call
+            self._misfit(cache, S)
+        n = S * d
+        qs = d if q.dtype is dt and q.is_contiguous() and q.numel() == n else self._rows(q, S)
+        os_ = d if out.dtype is dt and out.is_contiguous() and out.numel() == n else self._rows(out, S)
         if k_t is not None:
-            kp = k_t.data_ptr()
-            if S > 1:
-                ks = k_t.stride(0)
+            kp, ks = k_t.data_ptr(), d if k_t.dtype is dt and k_t.is_contiguous() and k_t.numel() == n else self._rows(k_t, S)
         if v_t is not None:
-            vp = v_t.data_ptr()
-            if S > 1 and k_t is not None and v_t.stride(0) != ks:
-                raise RTError("RT_ERR_INVALID_ARG", "k_t and v_t have one stride")
-        rc = self._L.rt_paged_attention(self._ctx, cache, S, lens.data_ptr(), max_len, q.data_ptr(), qs, kp, vp, ks, out.data_ptr(), os_,
-                                        None if lse is None else lse.data_ptr())
+            vp, vs = v_t.data_ptr(), d if v_t.dtype is dt and v_t.is_contiguous() and v_t.numel() == n else self._rows(v_t, S)
+            if vs != ks and kp is not None:
+                _invalid("k_t and v_t have one stride")
+        if lse is not None:
+            lp = lse.data_ptr()
+            if lse.dtype is not f32 or lse.numel() < S * H or not lse.is_contiguous():
+                _invalid("lse is contiguous float32 [S, n_heads]")
+        if lens.dtype is not i32 or lens.numel() < S or not lens.is_contiguous():
+            _invalid(_INTS)
+        rc = self._L.rt_paged_attention(self._ctx, cache, S, lens.data_ptr(), max_len, q.data_ptr(), qs, kp, vp, ks, out.data_ptr(), os_, lp)
         if rc:
             _check(self._L, self._ctx, rc)
 
     # -- rt_decode_step_paged(ctx, w, cache, x_t[S,d], S, pos[S] int32, max_pos, y_t[S,d])
     def rt_decode_step_paged(self, weights: rt_layer_weights, cache: rt_paged_cache, x_t, pos, max_pos, y_t):
-        rc = self._L.rt_decode_step_paged(self._ctx, weights, cache, x_t.data_ptr(), x_t.shape[0], pos.data_ptr(), max_pos, y_t.data_ptr())
+        dt, i32, _, d, _, most, fits = self._known or self._storage()
+        S = x_t.shape[0]
+        fit, lines = cache.fit
+        if (fit not in fits or S > lines) and S <= most:   # more than max_batch are refused by the call
+            self._misfit(cache, S)
+        if x_t.dtype is not dt or y_t.dtype is not dt or not x_t.is_contiguous() or not y_t.is_contiguous() or x_t.numel() != S * d \
+                or y_t.numel() < S * d:
+            _invalid("x_t and y_t are contiguous [S, d_model] of the storage dtype")
+        if pos.dtype is not i32 or pos.numel() < S or not pos.is_contiguous():
+            _invalid(_INTS)
+        rc = self._L.rt_decode_step_paged(self._ctx, weights, cache, x_t.data_ptr(), S, pos.data_ptr(), max_pos, y_t.data_ptr())
         if rc:
             _check(self._L, self._ctx, rc)
 
     # -- rt_lm_head_mx4(ctx, codes[vocab,d/2], exps[vocab,d/32], g_final[d] | None, vocab, z rows, z_stride, B, logits[B,vocab] f32)
     def rt_lm_head_mx4(self, codes, exps, g_final, z, z_stride, B, logits):
-        rc = self._L.rt_lm_head_mx4(self._ctx, codes.data_ptr(), exps.data_ptr(), None if g_final is None else g_final.data_ptr(),
-                                    codes.shape[0], z.data_ptr(), z_stride, B, logits.data_ptr())
+        dt, _, f32, d, _, _, _ = self._known or self._storage()
+        (vocab, half), gp = codes.shape, None
+        if half * 2 != d or exps.numel() != vocab * (d // 32) or codes.element_size() != 1 or not (codes.is_contiguous() and exps.is_contiguous()):
+            _invalid("codes [vocab, d / 2] and exps [vocab, d / 32] are contiguous bytes")
+        if z.dtype is not dt or not (z.numel() >= (B - 1) * z_stride + d if z.is_contiguous() else
+                                     z.shape[0] >= B and z.shape[-1] == d and z.stride(-1) == 1 and (z.stride(0) == z_stride or B == 1)):
+            _invalid("z is [B, d] of the storage dtype, its rows contiguous and z_stride apart")
+        if logits.dtype is not f32 or logits.numel() < B * vocab or not logits.is_contiguous():
+            _invalid("logits are contiguous float32 [B, vocab]")
+        if g_final is not None:
+            gp = g_final.data_ptr()
+            if g_final.dtype is not dt or g_final.numel() != d or not g_final.is_contiguous():
+                _invalid("g_final is [d] of the storage dtype")
+        rc = self._L.rt_lm_head_mx4(self._ctx, codes.data_ptr(), exps.data_ptr(), gp, vocab, z.data_ptr(), z_stride, B, logits.data_ptr())
         if rc:
             _check(self._L, self._ctx, rc)
 
