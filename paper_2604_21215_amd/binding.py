@@ -191,7 +191,7 @@ def make_weights(w: dict) -> rt_layer_weights:
     return s
 
 
-_INTS = "lengths, positions and counts are contiguous int32, one for each sequence"
+_INTS = "lengths, positions and counts are contiguous int32 on the context's device, one for each sequence"
 
 
 def _invalid(msg):
@@ -391,7 +391,7 @@ class RTContext:
         cfg = self.cfg
         H, size = cfg.n_heads, 2 if cfg.dtype == RT_BF16 else 4
         self._known = (torch.bfloat16 if size == 2 else torch.float32, torch.int32, torch.float32, cfg.d_model, H, cfg.max_batch,
-                       (0, _fit(H, size, cfg.device), _fit(H, 1, cfg.device)))
+                       (0, _fit(H, size, cfg.device), _fit(H, 1, cfg.device)), cfg.device)
         return self._known
 
     def _misfit(self, cache, S):
@@ -411,15 +411,15 @@ class RTContext:
         _invalid("rows are [S, n_heads, 64] or [S, d_model] of the storage dtype, contiguous inside")
 
     def _pairs(self, cache, first, count, k, v):
-        dt, i32, _, _, H, _, fits = self._known or self._storage()
+        dt, i32, _, _, H, _, fits, dev = self._known or self._storage()
         shape, stride, cp = k.shape, k.stride(), None
         if v.stride() == stride and stride[2:] == (64, 1) and v.shape == shape and shape[3] == 64 and shape[2] == H:
             ss, ps, _, _ = stride
         else:
             ss, ps = _pair_strides(k, v, H)
         S = shape[0]
-        if k.dtype is not dt or v.dtype is not dt:
-            _invalid("k and v are of the storage dtype")
+        if k.dtype is not dt or v.dtype is not dt or k.get_device() != dev or v.get_device() != dev or first.get_device() != dev:
+            _invalid("k and v are of the storage dtype and, as first and count, on the context's device")
         fit, lines = cache.fit
         if fit not in fits or S > lines:
             self._misfit(cache, S)
@@ -427,7 +427,7 @@ class RTContext:
             _invalid(_INTS)
         if count is not None:
             cp = count.data_ptr()
-            if count.dtype is not i32 or count.numel() < S or not count.is_contiguous():
+            if count.dtype is not i32 or count.numel() < S or not count.is_contiguous() or count.get_device() != dev:
                 _invalid(_INTS)
         return self._ctx, cache, S, first.data_ptr(), cp, shape[1], k.data_ptr(), v.data_ptr(), ss, ps
 
@@ -446,7 +446,7 @@ class RTContext:
     # -- rt_paged_attention(ctx, cache, S, lens[S] int32, max_len, q[S,H,64], q_stride, k_t | None, v_t | None, kv_stride, out, out_stride, lse[S,H] f32 | None)
     def rt_paged_attention(self, cache: rt_paged_cache, lens, max_len, q, k_t, v_t, out, lse=None):
         """q, k_t, v_t, out [S, H, 64] (or [S, d]): rows at their first stride, contiguous inside; lse [S, H]."""
-        dt, i32, f32, d, H, most, fits = self._known or self._storage()
+        dt, i32, f32, d, H, most, fits, dev = self._known or self._storage()
         S, kp, vp, lp, ks = q.shape[0], None, None, None, d
         fit, lines = cache.fit
         if (fit not in fits or S > lines) and S <= most:   # more than max_batch are refused by the call
@@ -462,17 +462,19 @@ class RTContext:
                 _invalid("k_t and v_t have one stride")
         if lse is not None:
             lp = lse.data_ptr()
-            if lse.dtype is not f32 or lse.numel() < S * H or not lse.is_contiguous():
-                _invalid("lse is contiguous float32 [S, n_heads]")
+            if lse.dtype is not f32 or lse.numel() < S * H or not lse.is_contiguous() or lse.get_device() != dev:
+                _invalid("lse is contiguous float32 [S, n_heads] on the context's device")
         if lens.dtype is not i32 or lens.numel() < S or not lens.is_contiguous():
             _invalid(_INTS)
+        if lens.get_device() != dev or q.get_device() != dev or out.get_device() != dev or (kp and k_t.get_device() != dev) or (vp and v_t.get_device() != dev):
+            _invalid("tensors lie on the context's device")
         rc = self._L.rt_paged_attention(self._ctx, cache, S, lens.data_ptr(), max_len, q.data_ptr(), qs, kp, vp, ks, out.data_ptr(), os_, lp)
         if rc:
             _check(self._L, self._ctx, rc)
 
     # -- rt_decode_step_paged(ctx, w, cache, x_t[S,d], S, pos[S] int32, max_pos, y_t[S,d])
     def rt_decode_step_paged(self, weights: rt_layer_weights, cache: rt_paged_cache, x_t, pos, max_pos, y_t):
-        dt, i32, _, d, _, most, fits = self._known or self._storage()
+        dt, i32, _, d, _, most, fits, dev = self._known or self._storage()
         S = x_t.shape[0]
         fit, lines = cache.fit
         if (fit not in fits or S > lines) and S <= most:   # more than max_batch are refused by the call
@@ -482,13 +484,15 @@ class RTContext:
             _invalid("x_t and y_t are contiguous [S, d_model] of the storage dtype")
         if pos.dtype is not i32 or pos.numel() < S or not pos.is_contiguous():
             _invalid(_INTS)
+        if pos.get_device() != dev or x_t.get_device() != dev or y_t.get_device() != dev:
+            _invalid("tensors lie on the context's device")
         rc = self._L.rt_decode_step_paged(self._ctx, weights, cache, x_t.data_ptr(), S, pos.data_ptr(), max_pos, y_t.data_ptr())
         if rc:
             _check(self._L, self._ctx, rc)
 
     # -- rt_lm_head_mx4(ctx, codes[vocab,d/2], exps[vocab,d/32], g_final[d] | None, vocab, z rows, z_stride, B, logits[B,vocab] f32)
     def rt_lm_head_mx4(self, codes, exps, g_final, z, z_stride, B, logits):
-        dt, _, f32, d, _, _, _ = self._known or self._storage()
+        dt, _, f32, d, _, _, _, dev = self._known or self._storage()
         (vocab, half), gp = codes.shape, None
         if half * 2 != d or exps.numel() != vocab * (d // 32) or codes.element_size() != 1 or not (codes.is_contiguous() and exps.is_contiguous()):
             _invalid("codes [vocab, d / 2] and exps [vocab, d / 32] are contiguous bytes")
@@ -501,6 +505,9 @@ class RTContext:
             gp = g_final.data_ptr()
             if g_final.dtype is not dt or g_final.numel() != d or not g_final.is_contiguous():
                 _invalid("g_final is [d] of the storage dtype")
+        if codes.get_device() != dev or exps.get_device() != dev or z.get_device() != dev or logits.get_device() != dev \
+                or (gp and g_final.get_device() != dev):
+            _invalid("tensors lie on the context's device")
         rc = self._L.rt_lm_head_mx4(self._ctx, codes.data_ptr(), exps.data_ptr(), gp, vocab, z.data_ptr(), z_stride, B, logits.data_ptr())
         if rc:
             _check(self._L, self._ctx, rc)

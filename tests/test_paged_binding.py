@@ -164,3 +164,29 @@ def test_read_out_refuses():
               dict(z=_bf16(S - 1, D)), dict(stride=2 * D), dict(z=_bf16(S, 2 * D)[:, :D]), dict(z=_bf16(D, S).t()), dict(logits=torch.zeros((S, vocab)).bfloat16()),
               dict(logits=torch.zeros((S, vocab - 1))), dict(logits=torch.zeros((vocab, S)).t())):
         _refused(ctx, lambda: go(**k))
+
+
+def test_tensors_of_another_device_are_refused():
+    """Every tensor of a call but one on the context's device (here the host)."""
+    vocab, u8 = 10, lambda *s: torch.zeros(s, dtype=torch.uint8)  # noqa: E731
+    z, w = torch.zeros((S, H)), binding.rt_layer_weights()
+    calls = (("rt_cache_write", lambda: [_i32(S), _i32(S), _bf16(S, 5, H, 64), _bf16(S, 5, H, 64)]),
+             ("rt_cache_read", lambda: [_i32(S), _i32(S), _bf16(S, 5, H, 64), _bf16(S, 5, H, 64)]),
+             ("rt_paged_attention", lambda: [_i32(S), 20, _bf16(S, H, 64), _bf16(S, H, 64), _bf16(S, H, 64), _bf16(S, H, 64), z]),
+             ("rt_decode_step_paged", lambda: [_bf16(S, D), _i32(S), 20, _bf16(S, D)]),
+             ("rt_lm_head_mx4", lambda: [u8(vocab, D // 2), u8(vocab, D // 32), _bf16(D), _bf16(S, D), D, S, torch.zeros((S, vocab))]))
+
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 1
+
+    for name, args in calls:
+        ctx, c = _ctx(), _cache()
+        before = {"rt_lm_head_mx4": [], "rt_decode_step_paged": [w, c]}.get(name, [c])
+        getattr(ctx, name)(*before, *args())
+        assert len(ctx.calls) == 1
+        for i, a in enumerate(args()):
+            if torch.is_tensor(a):
+                moved = args()
+                moved[i] = a.as_subclass(Elsewhere)
+                _refused(ctx, lambda: getattr(ctx, name)(*before, *moved), "device")
