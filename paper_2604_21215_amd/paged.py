@@ -19,7 +19,7 @@ class PagedCaches:
         if bits not in (0, 8):
             raise ValueError("bits is 0 (the storage dtype) or 8")
         per = -(-max_len // page_len)
-        self.page_len, self.max_len, self.bits = page_len, max_len, bits
+        self.page_len, self.max_len, self.bits, self.n_heads, self.dtype = page_len, max_len, bits, n_heads, dtype
         self.host_table = torch.full((places, per), -1, dtype=torch.int32)   # -1: no page
         self.table = self.host_table.to(device)
         self.free = list(range(pages - 1, -1, -1))

@@ -79,6 +79,11 @@ class DeviceStack:
     def _check_caches(self, caches: PagedCaches, S: int):
         if len(caches.layer) != len(self.layers) or S > len(caches.held):
             raise ValueError("caches of %d layers and at least %d places are required" % (len(self.layers), S))
+        # the kernels address the pools by the stack's heads and type
+        if caches.n_heads != self.H or (not caches.bits and torch_dtype(caches.dtype) != torch_dtype(self.dtype)) \
+                or caches.table.device != self.embedding.device:
+            raise ValueError("the caches hold %d heads in %s on %s, the stack has %d in %s on %s" % (
+                caches.n_heads, "8 bits" if caches.bits else caches.dtype, caches.table.device, self.H, self.dtype, self.embedding.device))
 
     def into_pages(self, caches: PagedCaches, lens):
         """The pairs that the last prefill (and the decode_steps behind it) left in self.K, self.V, rows 0 .. lens[b] - 1 of sequence b, into
