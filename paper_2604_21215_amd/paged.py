@@ -2,7 +2,8 @@
 
 A sequence has a place (a row of the table).  Pages are given out on the host, one number for the same page of every layer's pool; the
 rows in them are written and read by the library's kernels only.  reserve and release copy the table to the device on torch's current
-stream: that is the stream of the context that reads it, or one that the caller orders with it."""
+stream and return when it is there: that is the stream of the context that reads it, or one that the caller orders after the calls that
+still read it (a step in flight may lose the pages that release takes from it).  The pools are whole when __init__ returns."""
 from __future__ import annotations
 
 import torch
@@ -31,6 +32,8 @@ class PagedCaches:
         self.K_exp = [torch.zeros(shape[:3], dtype=torch.uint8, device=device) if bits else None for _ in range(layers)]
         self.V_exp = [torch.zeros(shape[:3], dtype=torch.uint8, device=device) if bits else None for _ in range(layers)]
         self.layer = [binding.make_cache(self.K[l], self.V[l], self.table, self.K_exp[l], self.V_exp[l]) for l in range(layers)]
+        if self.table.is_cuda:
+            torch.cuda.current_stream(self.table.device).synchronize()   # the fills: any stream's context may use the pools from here on
 
     def reserve(self, lengths) -> None:
         """Pages for positions 0 .. lengths[s] - 1 of every place s (a length below what a place holds changes nothing; places past the
