@@ -116,14 +116,14 @@ class DeviceStack:
 
     def into_pages(self, caches: PagedCaches, lens):
         """The pairs that the last prefill (and the decode_steps behind it) left in self.K, self.V, rows 0 .. lens[b] - 1 of sequence b, into
-        the pages of place b (which are reserved here, with room for the next token).  One length for each sequence of the prefill;
+        the pages of place b (which are reserved here, with room for the next token where max_len has it).  One length for each sequence of the prefill;
         lens[b] < 0: nothing of sequence b."""
         lens = [int(n) for n in lens]
         if self.K is None or len(lens) != self.K[0].shape[1] or max(lens) > self.K[0].shape[0]:
             raise ValueError("one length, of at most kv_cap, for each sequence of a prefill")
         self._check_caches(caches, len(lens))
         with self._on_context_stream():
-            caches.reserve([n + 1 if n >= 0 else 0 for n in lens])
+            caches.reserve([max(n, min(n + 1, caches.max_len)) if n >= 0 else 0 for n in lens])
             count = torch.tensor([max(n, 0) for n in lens], dtype=torch.int32, device=self.device)
             first = torch.tensor([0 if n >= 0 else -1 for n in lens], dtype=torch.int32, device=self.device)
             N = max(max(lens), 1)

@@ -60,3 +60,14 @@ def test_other_caches_are_refused(dtype, bits):
     with pytest.raises(ValueError, match="meta"):
         ds.into_pages(c, [4, 0, 9])
     assert not calls
+
+
+def test_a_sequence_that_fills_its_place_moves_into_pages():
+    ds, calls = _stack(2, "bf16", cap=MOST + 6)
+    c = PagedCaches(LAYERS, 2, ROWS, MOST, 12, page_len=16, dtype="bf16", device="cpu")
+    ds.into_pages(c, [MOST, MOST - 1, 0])
+    assert c.held == [4, 4, 1] and [n for n, _ in calls] == ["rt_cache_write"] * LAYERS
+    c = PagedCaches(LAYERS, 2, ROWS, MOST, 12, page_len=16, dtype="bf16", device="cpu")
+    with pytest.raises(ValueError):
+        ds.into_pages(c, [MOST + 1, 0, 0])
+    assert len(c.free) == 12 and len(calls) == LAYERS
