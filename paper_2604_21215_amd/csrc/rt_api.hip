@@ -1395,7 +1395,7 @@ static rt_status decode_paged(rt_ctx *c, LayerDims D, const rt_layer_weights *w,
     hipStream_t st = c->stream;
     Scratch S = c->S;
     S.Q = nullptr;   // the queries and the temporary pairs stay in fp32 rows
-    const bool mm = sizeof(T) == 2 && step_mm_supported(D, c->use_mfma) && !paged_products_take(D), wide = mm && step_uses_wide(D);
+    const bool mm = sizeof(T) == 2 && step_mm_supported(D, c->use_mfma) && !paged_products_take(D.B, D.d), wide = mm && step_uses_wide(D);
     const bool alus = (c->cfg.flags & RT_FLAG_NO_MFMA) != 0;
     if (wide) RT_TRY(step_qkv_wide(D, W, S, x_t, (size_t)D.d, st), "step_qkv_wide");
     else if (mm) RT_TRY(step_qkv_mm(D, W, S, x_t, (size_t)D.d, st), "step_qkv_mm");

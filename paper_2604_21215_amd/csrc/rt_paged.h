@@ -46,7 +46,6 @@ template <typename T>
 hipError_t paged_finish_launch(const PagedCache &C, const LayerDims &D, const int32_t *pos, int max_pos, const float *kv, const void *g_k,
                                const void *y_new, void *y, hipStream_t st);
 // The products of a step for the widths and types that step_mm_supported leaves out, and for batches they take (rt_paged_products.hip).
-bool paged_products_take(const LayerDims &D);
 template <typename T> hipError_t paged_qkv_launch(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, hipStream_t st);
 template <typename T>
 hipError_t paged_base_case_launch(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, void *y_new, hipStream_t st);

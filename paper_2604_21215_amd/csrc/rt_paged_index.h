@@ -115,4 +115,14 @@ RT_BOTH SplitPlan split_plan(int max_len, int S, int H, bool eight_bits)
     return p;
 }
 
+// The products of a step.  Where both kinds can run: those of rt_paged_products.hip read the rows as fp32 and start 16 outputs by 16 rows at a
+// time, the stack engine's prepare operand rows in one product for the next.  MI355X, us per step (up to 500 cached positions, bf16), these /
+// the others: d = 1024, 1 row 39.1 / 35.2, 4 rows 41.3 / 42.5, 8 43.9 / 51.1, 16 48.8 / 63.6, 32 56.8 / 76.1, 64 66.7 / 70.6, 128 101 / 82,
+// 200 157 / 108;  d = 512, 1 row 28.6 / 28.1, 8 31.3 / 35.1, 32 36.1 / 45.6, 128 51.5 / 57.2, 200 71.4 / 63.1;  d = 256, 4 rows 27.2 / 27.0,
+// 16 30.4 / 33.4, 200 47.4 / 49.4.
+RT_BOTH bool paged_products_take(int B, int d) { return B >= 8 && (int64_t)B * d <= 65536; }
+// Tiles of 16 outputs that a workgroup of rt_paged_products.hip owns: four share the splitting of their input rows, but only where that leaves
+// every compute unit a workgroup.
+RT_BOTH int paged_product_tiles(int n_out, int B) { return (int64_t)((n_out + 63) / 64) * ((B + 15) / 16) >= 256 ? 4 : 1; }
+
 }  // namespace rt

@@ -167,16 +167,10 @@ static void product(const void *Wa, const void *Wb, const void *Wc, int n_first,
     hipLaunchKernelGGL((paged_product_kernel<T, IN_T, EPI, NO>), dim3((n_out + 16 * NO - 1) / (16 * NO), cols), dim3(512), 0, st, (const T *)Wa, \
                        (const T *)Wb, (const T *)Wc, n_first, n_out, K, in, D.B, (const T *)gain, D.eps, do_norm, D.alpha, (const T *)res_T, \
                        res_f, out_f, (T *)out_T)
-    if ((n_out + 63) / 64 * cols >= 256) RT_PRODUCT(4);
+    if (paged_product_tiles(n_out, D.B) == 4) RT_PRODUCT(4);
     else RT_PRODUCT(1);
 #undef RT_PRODUCT
 }
-
-// Where both kinds can run: these read the rows as fp32 and start 16 outputs by 16 rows at a time, the stack engine's prepare operand rows in
-// one product for the next.  MI355X, us per step (up to 500 cached positions, bf16), these / the others: d = 1024, 1 row 39.1 / 35.2, 4 rows 41.3 / 42.5,
-// 8 43.9 / 51.1, 16 48.8 / 63.6, 32 56.8 / 76.1, 64 66.7 / 70.6, 128 101 / 82, 200 157 / 108;  d = 512, 1 row 28.6 / 28.1, 8 31.3 / 35.1, 32 36.1 / 45.6,
-// 128 51.5 / 57.2, 200 71.4 / 63.1;  d = 256, 4 rows 27.2 / 27.0, 16 30.4 / 33.4, 200 47.4 / 49.4.
-bool paged_products_take(const LayerDims &D) { return D.B >= 8 && (long long)D.B * D.d <= 65536; }
 
 // raw [q | k_tmp | v_tmp] of x_t [B][d] into S.qkv_raw
 template <typename T> hipError_t paged_qkv_launch(const LayerDims &D, const Weights &W, const Scratch &S, const void *x_t, hipStream_t st)
