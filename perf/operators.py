@@ -114,7 +114,7 @@ def _pool(g, case, H, pages, filled):
 def prepare(case, seed):
     g = torch.Generator(device=DEVICE)
     g.manual_seed(int(seed))
-    kind, s = case["kind"], dict(case=case)
+    kind, s = case["kind"], dict(case=case, stream=torch.cuda.current_stream().cuda_stream)
     if kind == "readout":
         d, B = case["d"], case["B"]
         # what is packed ahead: codes of two weights a byte, the even index in the low half, and one exponent byte per block of 32
@@ -160,16 +160,21 @@ def prepare(case, seed):
 
 
 # ---------------------------------------------------------------------------------------------- the library's calls
-_contexts = {}
+_contexts, MOST_CONTEXTS = {}, 64
 
 
-def _context(case, binding):
-    """The context that a server keeps for its layers: one per shape, whatever the batch in hand holds."""
+def _context(s, binding):
+    """The context that a server keeps for its layers: one per shape and stream, whatever the batch in hand holds.  A state is run on the
+    stream that it was prepared on."""
+    case = s["case"]
     d, rows = case.get("d") or 64 * case["H"], case.get("S") or case["B"]
-    key = (d, rows, case["dtype"], case.get("alibi", 0.0), case.get("scale", 1.0))
+    key = (d, rows, case["dtype"], case.get("alibi", 0.0), case.get("scale", 1.0), s["stream"])
     if key not in _contexts:
+        if len(_contexts) >= MOST_CONTEXTS:   # the oldest goes, when the device is done with it
+            torch.cuda.synchronize()
+            _contexts.pop(next(iter(_contexts))).rt_destroy()
         _contexts[key] = binding.RTContext(d, d // 64, 4 * d, rows, 1, case["dtype"], attn_scale=key[4], rms_eps=EPS, alibi_max_bias=key[3],
-                                           stream=torch.cuda.current_stream().cuda_stream, reserve=binding.RT_RESERVE_PAGED)
+                                           stream=s["stream"], reserve=binding.RT_RESERVE_PAGED)
     return _contexts[key]
 
 
@@ -177,7 +182,7 @@ def _run_own(s):
     from paper_2604_21215_amd import binding
 
     case = s["case"]
-    ctx, kind = _context(case, binding), case["kind"]
+    ctx, kind = _context(s, binding), case["kind"]
     if kind == "readout":
         ctx.rt_lm_head_mx4(s["codes"], s["exps"], s["g_final"], s["z"], case["d"], case["B"], s["logits"])
         return s["logits"]
