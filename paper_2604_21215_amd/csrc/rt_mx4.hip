@@ -121,9 +121,11 @@ __device__ __forceinline__ void eight(const uint4 (&r)[2], float (&f)[8])
 // lane and slice, turns them into four fragments and feeds 4 CT PARTS matrix instructions.  The slices' partial tiles meet in LDS, RT tiles at
 // a time, and are summed in slice order; the row's 1 / rms is applied to the sum.  No element of z is read or split twice by a workgroup, and
 // nothing but partial tiles goes through LDS.
-// Bound: for few rows the matrix (17 bytes per 32 weights; one row, d = 1024, 32768 vocabulary rows: 7.8 us = 2.3 TB/s, of which some 4 us are
+// Bound: for few rows the matrix (17 bytes per 32 weights; one row, d = 1024, 32768 vocabulary rows: 8.5 us = 2.1 TB/s, of which some 4 us are
 // the launch and the first trip to memory); for 64 rows the chain of loads, conversions, products and sums that the two wavefronts of a SIMD
-// walk through (50001 vocabulary rows: 23.7 us; with rows staged in LDS and the matrix read once per 16 rows 187).
+// walk through (50001 vocabulary rows: 24.1 us, the matrix units busy for 22 % of it; with rows staged in LDS and the matrix read once per 16
+// rows 187).  Every further batch tile of 16 CT rows reads the matrix again: 128 rows 43.3 us, 200 78.6; fp32, 64 rows (two tiles) 55.3, 200 162;
+// 64 rows of d = 2048 (two tiles) 58.8, of 4096 (four) 265.
 // 32 columns and twice the wavefronts: 32 us; two tiles per barrier at 64 columns: 24.6.
 // grid (<= groups of RT tiles, batch tiles of 16 CT), block 64 NW.
 template <typename T, int PARTS, int CT, int SL, int RT, int WMAX>
@@ -339,7 +341,9 @@ static hipError_t mx4_rows_go(const uint8_t *codes, const uint8_t *exps, const T
     return hipGetLastError();
 }
 
-// ---- rows too wide for registers: staged in LDS as three parts, a tile of rows at a time.
+// ---- rows too wide for registers (d > 4096, fp32 > 2048) or off 16 bytes: staged in LDS as three parts, a tile of rows at a time.
+// Bound: the chain of LDS reads and products of one wavefront's tile; 32768 vocabulary rows: one bf16 row of d = 8192 155 us (the matrix at 0.9
+// TB/s), 16 rows 936 (three to a tile), one fp32 row of d = 4096 64.
 // grid (<= row tiles / 4, batch tiles of bt), block 256, LDS 3 bt ld bf16.
 constexpr size_t kMxMaxLds = 152 * 1024;
 

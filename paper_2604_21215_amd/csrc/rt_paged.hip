@@ -82,8 +82,9 @@ __device__ __forceinline__ int row_position(const PairRows &R, int s, int n, lon
 
 // One row of one head per 4, 8 or 16 lanes, its keys and its values.  Rows of a workgroup: tiles of eight consecutive positions (one where
 // a call has fewer), head after head, so that both the 128 bytes of a head read and the runs of a page written are neighbours.
-// Bound: memory (eight prompts of up to 2048 positions, 16 heads, to 8 bits: 44 MB in 9.3 us = 4.8 TB/s, the rate of a large copy; back the
-// same).  grid (row groups, S), block 256.
+// Bound: memory; a large copy reaches 4.9 TB/s.  16 heads, over three sets of rows in turn, write / read: 8 sequences of 2048 positions in bf16
+// (134 MB) 30.5 us = 4.4 TB/s / 28.5 = 4.7, bf16 and 8 bits (101 MB) 24.3 = 4.2 / 25.8 = 3.9, fp32 (268 MB) 54.3 = 4.9 / 52.7 = 5.1, fp32 and
+// 8 bits (168 MB) 38.8 = 4.3 / 44.1 = 3.8; four times as many sequences 4.3 to 4.6 / 4.3 to 5.3 TB/s.  grid (row groups, S), block 256.
 template <typename T, bool BITS8, int TILE>
 __global__ __launch_bounds__(256) void cache_write_kernel(const PagedCache C, const PairRows R, int H, const T *__restrict__ k,
                                                           const T *__restrict__ v)
@@ -272,12 +273,15 @@ __device__ __forceinline__ void finish_row(const PagedAttention &A, int s, int h
 
 // C: type of the cached values (T or int8_t).  Workgroup = (h, s, split), heads first: consecutive workgroups go to different XCDs, and all
 // heads of a sequence have the same work, while the late splits of a ragged batch are mostly empty (splits first, and eight of them: an
-// XCD gets one split of every sequence, 512 pairs of up to 8000 positions: 125 us instead of 98).  Its wavefronts share the split's rows in as many runs.
+// XCD gets one split of every sequence, 512 pairs of up to 8000 positions: 125 us instead of 98).  Its wavefronts share the split's rows in
+// as many runs.
 // A wavefront loads 64 rows of keys and of values (fp32: 32), or 16 where no more are left, before it computes on them; the other wavefronts of
 // its SIMD cover the trip (a second chunk on the way in registers leaves two wavefronts a SIMD and is slower: 8 bits, 64 sequences of up to
 // 2000: 28 -> 31 us).
-// Bound: memory.  200 sequences of up to 4096 positions, 16 heads, bf16: 1.67 GB in 281 us = 5.9 TB/s; 64 of up to 2000 in 8 bits: 131 MB in
-// 27 us = 4.9 TB/s; one of 37: 3.5 us, three dependent trips.
+// Bound: memory, and for ragged batches of few sequences the longest of them.  16 heads, over three sets of pages in turn: 200 sequences of up
+// to 4096 positions in bf16, 1.63 GB in 281 us = 5.8 TB/s, in 8 bits 868 MB in 188 = 4.6; 64 of up to 2000 in 8 bits 123 MB in 34.9 = 3.5,
+// all of 2000 266 MB in 58.9 = 4.5 (in bf16 4.5 and 5.3, in fp32 4.5 and 5.5).  What the last-level cache holds is faster: that one set again
+// and again 28.1.  One sequence of 37: 4.1 us, three dependent trips.
 template <typename T, typename C, bool STEP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void paged_attention_kernel(const PagedCache P, const PagedAttention A)
 {
@@ -305,7 +309,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attention_kernel(const Paged
     }
     if (lo >= n && !one) return;   // no rows here; the join counts the splits in the same way
     const int hi = min(n, lo + A.plan.split_len);
-    // this wavefront's run: a quarter of the rows, in whole chunks where there is more than one for each
+    // this wavefront's run: its share of the rows, in whole chunks where there is more than one for each
     const int unit = hi - lo > WAVES * 16 ? CH : 16;
     const int share = ((hi - lo + WAVES * unit - 1) / (WAVES * unit)) * unit;
     const int wlo = lo + wave * share, whi = min(hi, wlo + share);

@@ -77,13 +77,20 @@ RT_BOTH int row_code(float u, int byte)   // the code of a value (clipped, if th
 //   parts of about kLong, which bounds how long one sequence of a ragged batch keeps its workgroup after the others are done.
 //   Many pairs, long rows in the storage dtype (kMany16 positions, between the 2000 and the 4000 measured below): sixteen
 //   wavefronts again, which end their sequences four times as early.
-// MI355X, us per call, S H pairs of up to so many positions, waves * parts (bf16 unless said):
+// MI355X, us per call on the same inputs again and again, S H pairs of up to so many positions, waves * parts (bf16 unless said):
 //   16 pairs, 500: 4*1 6.0, 16*1 5.6;  1000: 4*1 8.7, 4*4 7.7, 16*1 7.3;  2000: 4*1 14.3, 4*8 7.8, 16*1 10.5;  14 pairs, 513, fp32: 4*1 7.7, 16*1 5.8;
 //   64 pairs, 1000: 4*4 8.0, 16*1 7.3;  2000: 4*8 8.6, 16*1 10.6;  8000: 4*1 62, 4*16 17.6, 16*4 17.0;
 //   256 pairs, 500: 4*1 6.2, 16*1 5.9;  1000: 4*1 10.6, 16*1 8.1;  2000: 4*4 18.1, 16*1 14.8;  4000: 4*8 26.6, 16*1 24.0;  8000: 4*8 44, 16*1 44;
 //   512 pairs, 500: 4*1 9.8, 16*1 11.4;  2000: 4*1 27.8, 4*4 29.7, 16*1 26.3;  768 pairs, 1000: 4*1 20.1, 16*1 20.5;  4000: 4*4 76.8, 16*1 71.0;
 //   1024 pairs, 2000, 8 bits: 4*1 28.5, 16*1 33.3;  3200 pairs, 4096: 4*1 298, 4*4 294, 16*1 281;  8 bits: 4*1 184, 4*4 177, 16*1 193;
 //   1600 pairs, 8000, 8 bits: 4*1 188, 4*8 160, 16*1 176;  32 pairs, 100001: 4*1 1015, 4*8 152, 4*32 118, 4*64 117, 16*8 111.
+// In 8 bits, few pairs: 16 pairs, 500: 4*1 6.0, 16*1 6.0;  1000: 4*1 8.3, 4*4 7.6, 16*1 7.6;  2000: 4*1 12.8, 4*8 7.8, 16*1 10.8;
+//   128 pairs, 1000: 4*1 8.3, 16*1 7.6;  2000: 4*8 10.8, 16*1 11.0;  4000: 4*1 26.1, 4*8 15.0, 4*16 14.3, 16*1 18.1, 16*2 15.7;
+//   256 pairs, 1000: 4*1 8.5, 16*1 7.9;  2000: 4*1 15.2, 4*8 14.2, 16*1 11.9;  4000: 4*1 28.5, 4*8 21.1, 16*1 20.4;
+//   many pairs: 512, 4000: 4*1 33.7, 4*8 30.6, 16*1 30.1;  1024, 4000: 4*1 52.8, 4*4 48.3, 16*1 57.9.
+// fp32: 16 pairs, 300: 4*1 6.2, 16*1 5.6;  1000: 4*1 11.0, 4*4 8.4, 16*1 8.7;  2000: 4*1 18.3, 4*8 8.3, 16*1 13.3;
+//   256 pairs, 1000: 4*1 15.9, 16*1 14.1;  2000: 4*1 26.6, 16*1 23.7;  4000: 4*1 53, 4*16 45.9, 16*1 45.0;  320, 8000: 4*1 186, 4*8 150, 16*1 145;
+//   512 pairs, 2000: 4*1 52.1, 16*1 49.5;  3200: 4*1 92, 4*4 87, 16*1 88;  4000: 4*1 112, 4*4 106, 16*1 106, 16*2 101;  1024, 4000: 4*1 199, 4*4 188, 16*1 197.
 struct SplitPlan {
     int split_len, n_splits, waves;
 };
@@ -122,7 +129,9 @@ RT_BOTH SplitPlan split_plan(int max_len, int S, int H, bool eight_bits)
 // 16 30.4 / 33.4, 200 47.4 / 49.4.
 RT_BOTH bool paged_products_take(int B, int d) { return B >= 8 && (int64_t)B * d <= 65536; }
 // Tiles of 16 outputs that a workgroup of rt_paged_products.hip owns: four share the splitting of their input rows, but only where that leaves
-// every compute unit a workgroup.
+// every compute unit a workgroup.  us per step, by this rule / one tile everywhere / four: bf16, d = 1024, 32 rows 55.7 / 55.0 / 71.7, 64 rows 68.1 /
+// 74.3 / 79.1;  d = 320, 200 rows 54.4 / 56.9 / 54.6;  fp32, d = 1024, 64 rows 85.0 / 88.6 / 119.1, 128 rows 138 / 147 / 153;  but d = 576, 400 rows
+// 134 / 157 / 118, whose Wo and W2 just miss the line.
 RT_BOTH int paged_product_tiles(int n_out, int B) { return (int64_t)((n_out + 63) / 64) * ((B + 15) / 16) >= 256 ? 4 : 1; }
 
 }  // namespace rt
