@@ -213,7 +213,8 @@ def _fit(heads, size, device):
 
 
 def make_cache(K, V, table, K_exp=None, V_exp=None) -> rt_paged_cache:
-    """K, V [pages, H, page_len, 64] (storage dtype, or int8 with the bytes K_exp, V_exp [pages, H, page_len]), table int32 [S, entries]."""
+    """K, V [pages, H, page_len, 64] (storage dtype, or int8 with the bytes K_exp, V_exp [pages, H, page_len]), table int32 [S, entries],
+    contiguous: the kernels read whole lines, and follow any entry that a position leads to."""
     int8, uint8, int32 = _dtypes or _load_dtypes()
     shape, dt, dev, ke, ve = K.shape, K.dtype, K.get_device(), None, None
     pages, heads, page_len, width = shape if len(shape) == 4 else (0, 0, 0, 0)
@@ -226,13 +227,13 @@ def make_cache(K, V, table, K_exp=None, V_exp=None) -> rt_paged_cache:
             if t.dtype is not uint8 or t.shape != shape[:3] or not t.is_contiguous() or t.get_device() != dev:
                 _invalid("K_exp, V_exp are contiguous uint8 [pages, H, page_len] on the device of K")
         ke, ve = K_exp.data_ptr(), V_exp.data_ptr()
-    (lines, entries), (stride, inner) = table.shape, table.stride()
-    if table.dtype is not int32 or (inner != 1 and entries > 1):
-        _invalid("table is int32 [S, entries]")
+    lines, entries = table.shape
+    if table.dtype is not int32 or not table.is_contiguous():   # a line's entries are all that lie up to the next line
+        _invalid("table is contiguous int32 [S, entries]")
     if V.get_device() != dev or table.get_device() != dev:
         _invalid("K, V and table lie on one device")
     size = K.element_size()
-    c = rt_paged_cache(K.data_ptr(), V.data_ptr(), ke, ve, table.data_ptr(), stride if lines > 1 else entries, pages, page_len, 8 if size == 1 else 0)
+    c = rt_paged_cache(K.data_ptr(), V.data_ptr(), ke, ve, table.data_ptr(), entries, pages, page_len, 8 if size == 1 else 0)
     c.fit = heads << 16 | size << 12 | dev + 2, lines
     return c
 

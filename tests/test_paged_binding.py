@@ -73,9 +73,11 @@ def test_make_cache_refuses():
     K8, exp = K.to(torch.int8), torch.zeros((5, H, 16), dtype=torch.uint8)
     c = binding.make_cache(K, V, table)
     assert (c.pages, c.page_len, c.bits, c.table_stride) == (5, 16, 0, ENTRIES)
-    c = binding.make_cache(K8, K8.clone(), torch.zeros((S, 9), dtype=torch.int32)[:, :ENTRIES], exp, exp.clone())
+    c = binding.make_cache(K8, K8.clone(), torch.zeros((S + 1, 9), dtype=torch.int32)[:S], exp, exp.clone())
     assert (c.pages, c.page_len, c.bits, c.table_stride) == (5, 16, 8, 9)
     for args in ((K, V, table.float()), (K, V, table.long()), (K, V, torch.zeros((ENTRIES, S), dtype=torch.int32).t()),
+                 # columns of a wider table: its other columns would be followed, and read past the end behind the last line
+                 (K, V, torch.zeros((S, 9), dtype=torch.int32)[:, :ENTRIES]), (K, V, torch.zeros((S, 9), dtype=torch.int32)[:, 5:]),
                  (K, V[:4], table), (K, V.float(), table), (K.transpose(1, 2), V.transpose(1, 2), table), (K[..., :32], V[..., :32], table),
                  (K[..., :32].contiguous(), V[..., :32].contiguous(), table), (K8, K8, table), (K, V, table, exp, exp), (K8, K8, table, exp, None),
                  (K8, K8, table, None, exp), (K8, K8, table, exp, exp[:4]), (K8, K8, table, exp.int(), exp.int()), (K[0], V[0], table)):
