@@ -296,7 +296,7 @@ typedef struct {
     void *K, *V;              /* [pages][n_heads][page_len][head_dim]: storage dtype, or int8 codes (bits = 8); on 16 bytes */
     uint8_t *K_exp, *V_exp;   /* [pages][n_heads][page_len] bytes of a cache of 8 bits, else NULL */
     const int32_t *table;     /* [S][table_stride], all of it readable: entry i of sequence s is the page of positions i page_len .. + page_len - 1 */
-    int64_t table_stride;     /* entries; table_stride * page_len positions at most */
+    int64_t table_stride;     /* entries, 1 .. 2^26; table_stride * page_len positions at most, themselves at most 2^31 */
     int32_t pages;
     int32_t page_len;         /* a power of two, 16 .. 1024 */
     int32_t bits;             /* 0: storage dtype; 8 */

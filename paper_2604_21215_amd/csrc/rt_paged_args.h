@@ -50,6 +50,8 @@ inline rt_status check_pool(const rt_config &cfg, const rt_paged_cache *cache, i
         return RT_ERR_INVALID_ARG;
     *msg = "1 <= S <= 65535 and 1 <= table_stride <= 2^26 are required";
     if (S < 1 || S > 65535 || cache->table_stride < 1 || cache->table_stride > (1 << 26)) return RT_ERR_INVALID_ARG;
+    *msg = "a line of the table may name 2^31 positions at most";
+    if (cache->table_stride * cache->page_len > (int64_t)1 << 31) return RT_ERR_INVALID_ARG;
     *msg = "K and V of a cache must lie on 16 bytes";
     if (!on16(cache->K) || !on16(cache->V)) return RT_ERR_INVALID_ARG;
     const size_t rows = (size_t)cache->pages * (size_t)cfg.n_heads * (size_t)cache->page_len;

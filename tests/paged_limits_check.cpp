@@ -87,6 +87,14 @@ static int overlaps()
     EXPECT(check_pool(c, &inside, 3, &R, &msg) == RT_OK);
     inside.table = (const int32_t *)at((2ull << 40) - 80);
     EXPECT(check_pool(c, &inside, 3, &R, &msg) == RT_ERR_INVALID_ARG && check_pool(c, &inside, 2, &R, &msg) == RT_OK);
+    // positions are 32-bit numbers: the last one that a line may name is 2^31 - 1
+    rt_paged_cache wide = p;
+    wide.page_len = 1024; wide.table_stride = 1 << 21;
+    EXPECT(check_pool(c, &wide, 1, &R, &msg) == RT_OK);
+    wide.table_stride = (1 << 21) + 1;
+    EXPECT(check_pool(c, &wide, 1, &R, &msg) == RT_ERR_INVALID_ARG);
+    wide.page_len = 16; wide.table_stride = 1 << 26;
+    EXPECT(check_pool(c, &wide, 1, &R, &msg) == RT_OK);
     EXPECT(check_pool(c, &p, 3, &R, &msg) == RT_OK);
 
     char *k = at(7ull << 40), *v = at(8ull << 40), *q = at(9ull << 40), *out = at(10ull << 40);
