@@ -204,7 +204,7 @@ _dtypes = None
 def _load_dtypes():   # an import statement in a call costs as much as three of its checks
     global _dtypes
     import torch
-    _dtypes = torch.int8, torch.uint8, torch.int32
+    _dtypes = torch.int8, torch.uint8, torch.int32, {torch.int8: 1, torch.bfloat16: 2, torch.float32: 4}
     return _dtypes
 
 
@@ -215,11 +215,11 @@ def _fit(heads, size, device):
 def make_cache(K, V, table, K_exp=None, V_exp=None) -> rt_paged_cache:
     """K, V [pages, H, page_len, 64] (storage dtype, or int8 with the bytes K_exp, V_exp [pages, H, page_len]), table int32 [S, entries],
     contiguous: the kernels read whole lines, and follow any entry that a position leads to."""
-    int8, uint8, int32 = _dtypes or _load_dtypes()
+    int8, uint8, int32, sizes = _dtypes or _load_dtypes()
     shape, dt, dev, ke, ve = K.shape, K.dtype, K.get_device(), None, None
     pages, heads, page_len, width = shape if len(shape) == 4 else (0, 0, 0, 0)
-    if width != 64 or V.shape != shape or V.dtype is not dt or not (K.is_contiguous() and V.is_contiguous()):
-        _invalid("K, V are contiguous [pages, H, page_len, 64] of one type")
+    if width != 64 or V.shape != shape or V.dtype is not dt or dt not in sizes or not (K.is_contiguous() and V.is_contiguous()):
+        _invalid("K, V are contiguous [pages, H, page_len, 64] of one type: bfloat16, float32 or int8")
     if dt is int8 or K_exp is not None or V_exp is not None:
         if K_exp is None or V_exp is None or dt is not int8:
             _invalid("K_exp, V_exp belong to a cache of 8 bits (K, V int8), and to no other")
@@ -232,7 +232,7 @@ def make_cache(K, V, table, K_exp=None, V_exp=None) -> rt_paged_cache:
         _invalid("table is contiguous int32 [S, entries]")
     if V.get_device() != dev or table.get_device() != dev:
         _invalid("K, V and table lie on one device")
-    size = K.element_size()
+    size = sizes[dt]
     c = rt_paged_cache(K.data_ptr(), V.data_ptr(), ke, ve, table.data_ptr(), entries, pages, page_len, 8 if size == 1 else 0)
     c.fit = heads << 16 | size << 12 | dev + 2, lines
     return c
@@ -495,7 +495,8 @@ class RTContext:
     def rt_lm_head_mx4(self, codes, exps, g_final, z, z_stride, B, logits):
         dt, _, f32, d, _, _, _, dev = self._known or self._storage()
         (vocab, half), gp = codes.shape, None
-        if half * 2 != d or exps.numel() != vocab * (d // 32) or codes.element_size() != 1 or not (codes.is_contiguous() and exps.is_contiguous()):
+        if half * 2 != d or exps.numel() != vocab * (d // 32) or codes.element_size() != 1 or exps.element_size() != 1 \
+                or not (codes.is_contiguous() and exps.is_contiguous()):
             _invalid("codes [vocab, d / 2] and exps [vocab, d / 32] are contiguous bytes")
         if z.dtype is not dt or not (z.numel() >= (B - 1) * z_stride + d if z.is_contiguous() else
                                      z.shape[0] >= B and z.shape[-1] == d and z.stride(-1) == 1 and (z.stride(0) == z_stride or B == 1)):

@@ -75,7 +75,7 @@ def test_make_cache_refuses():
     assert (c.pages, c.page_len, c.bits, c.table_stride) == (5, 16, 0, ENTRIES)
     c = binding.make_cache(K8, K8.clone(), torch.zeros((S + 1, 9), dtype=torch.int32)[:S], exp, exp.clone())
     assert (c.pages, c.page_len, c.bits, c.table_stride) == (5, 16, 8, 9)
-    for args in ((K, V, table.float()), (K, V, table.long()), (K, V, torch.zeros((ENTRIES, S), dtype=torch.int32).t()),
+    for args in ((K.half(), V.half(), table), (K.to(torch.int16), V.to(torch.int16), table), (K.to(torch.int32), V.to(torch.int32), table), (K, V, table.float()), (K, V, table.long()), (K, V, torch.zeros((ENTRIES, S), dtype=torch.int32).t()),
                  # columns of a wider table: its other columns would be followed, and read past the end behind the last line
                  (K, V, torch.zeros((S, 9), dtype=torch.int32)[:, :ENTRIES]), (K, V, torch.zeros((S, 9), dtype=torch.int32)[:, 5:]),
                  (K, V[:4], table), (K, V.float(), table), (K.transpose(1, 2), V.transpose(1, 2), table), (K[..., :32], V[..., :32], table),
@@ -161,7 +161,7 @@ def test_read_out_refuses():
     for k in good:
         go(**k)
     assert len(ctx.calls) == len(good)
-    for k in (dict(codes=u8(vocab, D)), dict(codes=u8(vocab, D)[:, ::2]), dict(codes=torch.zeros((vocab, D // 2), dtype=torch.int32)), dict(exps=u8(vocab - 1, D // 32)),
+    for k in (dict(codes=u8(vocab, D)), dict(codes=u8(vocab, D)[:, ::2]), dict(codes=torch.zeros((vocab, D // 2), dtype=torch.int32)), dict(exps=u8(vocab - 1, D // 32)), dict(exps=torch.zeros((vocab, D // 32), dtype=torch.int32)),
               dict(exps=u8(D // 32, vocab).t()), dict(g=torch.zeros(D)), dict(g=_bf16(D - 1)), dict(g=_bf16(2 * D)[::2]), dict(z=torch.zeros((S, D))),
               dict(z=_bf16(S - 1, D)), dict(stride=2 * D), dict(z=_bf16(S, 2 * D)[:, :D]), dict(z=_bf16(D, S).t()), dict(logits=torch.zeros((S, vocab)).bfloat16()),
               dict(logits=torch.zeros((S, vocab - 1))), dict(logits=torch.zeros((vocab, S)).t())):
